@@ -368,6 +368,124 @@ DART_API double dart_score_tolerance(int32_t dtype);
 DART_API dart_status dart_probe_mfma_dot32(const void* A, const void* B, float* out,
                                            int32_t tiles, void* stream);
 
+/* ---- attention on either side of the step -------------------------------------------------
+ * The layers around the reduction step make the key rows whose norm step (a) ranks, and read the
+ * rows that are left after step (d).  The calls below are that part of a layer: queries and
+ * keys are normed and rotated by their position ids (which after the step are the carried ids
+ * of the retained tokens, in one or several planes), keys and values go to a paged cache, and
+ * attention reads the cache, for one new token of every sequence as for whole prompts.
+ * Memory, streams, errors and determinism are as described at the top of this file; what is
+ * checked on the device is reported in *status (see dart_cache).  Value range: any; infinities and
+ * NaN in a row that is seen go into the results they belong to and no others, and what lies in
+ * a page outside the keys of its sequence is never used.                                     */
+
+/* How the heads of a layer are normed and rotated (host memory, plain data).
+ * Element i of a head is x_i; with a weight, x is first replaced by
+ *   x_i * weight_i / sqrt(mean_j x_j^2 + eps).
+ * Pair p < rot/2 of a head, elements (p, p + rot/2), or (2p, 2p + 1) with interleaved, is then
+ * turned by theta = position * inv_freq[p] (the angle in 64 bits, its sine and cosine in 32):
+ *   (a, b) -> scale * (a cos - b sin, b cos + a sin);
+ * elements from rot on pass.  All in 32 bits, rounded once to the type of the rows.          */
+typedef struct dart_rotation {
+  int32_t Hq;          /* query heads of a row, a multiple of Hkv, <= 1024                   */
+  int32_t Hkv;         /* key heads (and value heads), >= 1                                  */
+  int32_t d;           /* elements of a head: a multiple of 8, <= 256                         */
+  int32_t dtype;       /* dart_dtype of rows, weights, outputs and pages                     */
+  int32_t rot;         /* elements of a head that are turned: a multiple of 8, 0..d          */
+  int32_t interleaved; /* 0: pairs (p, p + rot/2); 1: pairs (2p, 2p + 1)                     */
+  int32_t planes;      /* planes of position ids, 1..4                                       */
+  int32_t sections[4]; /* the first sections[0] pairs follow plane 0, the next sections[1]
+                          plane 1, ...; they sum to rot/2 (ignored when planes == 1)         */
+  const float* inv_freq; /* DEVICE float[rot/2]                                              */
+  const void* q_weight;  /* DEVICE [d], or NULL: queries are not normed                      */
+  const void* k_weight;  /* DEVICE [d], or NULL: keys are not normed                         */
+  float eps;             /* >= 0                                                             */
+  float scale;           /* factor of the turned elements (1 for plain rotations)            */
+} dart_rotation;
+
+/* Keys and values in pages, and the tokens of one call (host memory, plain data).  Key head h of
+ * row r of page p is the d elements from p*page_ld + h*head_ld + r*row_ld of the key pool, the value
+ * head likewise in the value pool; so pages may hold heads of rows (head_ld = page_size*row_ld) or
+ * rows of heads (row_ld = Hkv*head_ld), and one page as long as a sequence is a plain cache.
+ * Key j of sequence b is row j % page_size of page pages[b*pages_ld + j/page_size].
+ * Tokens are packed: sequence b owns tokens cu_q[b] .. cu_q[b+1]-1 of the call, and kv_len[b] keys
+ * of its own in the cache with this call's: its last n_b = cu_q[b+1] - cu_q[b] keys belong to
+ * the call's tokens, in order (dart_attend without `causal` does not ask for that).
+ * Shared prefixes (groups > 0): sequences group_cu[g] .. group_cu[g+1]-1 all see, before their own
+ * keys, the prefix_len[g] keys of the pages prefix_pages[g*prefix_ld + ...], which are stored and
+ * read once for all of them.
+ * A sequence whose offsets decrease or leave 0..T, with more than max_q tokens, whose kv_len is below 0
+ * or over max_kv or over pages_ld*page_size, or whose prefix is as wrong, is skipped: nothing is appended
+ * for it and its output is as if it saw no key; bit 0 of *status is set.  A page number outside
+ * 0..n_pages-1 where a key is needed sets bit 1: the key is not appended, or the sequence's
+ * output is unspecified.  status (DEVICE int32, or NULL) is only ever OR-ed into: the caller
+ * clears it.                                                                                  */
+typedef struct dart_cache {
+  int32_t B;        /* sequences, 0..2^20                                                     */
+  int32_t Hq, Hkv;  /* query heads, key/value heads: as dart_rotation                         */
+  int32_t d;        /* elements of a head: a multiple of 8, <= 256                            */
+  int32_t dtype;    /* dart_dtype of q, k, v, pools and out                                   */
+  int32_t T;        /* tokens of the call, 0..2^24                                            */
+  int32_t max_q;    /* host-known upper bound of every n_b                                    */
+  int32_t max_kv;   /* host-known upper bound of every kv_len, 0..2^27                        */
+  const int32_t* cu_q;   /* DEVICE int32[B+1] from 0 to T, or NULL: one token each (T == B)   */
+  const int32_t* kv_len; /* DEVICE int32[B]                                                   */
+  const int32_t* pages;  /* DEVICE int32[B][pages_ld]                                         */
+  int32_t pages_ld;      /* entries of a row of `pages`, >= 1                                 */
+  int32_t n_pages;       /* pages of the pools, >= 1                                          */
+  int32_t page_size;     /* rows of a page: a power of two, 1..2^20                           */
+  int64_t page_ld, head_ld, row_ld; /* strides in elements: multiples of 8 (of 4 for 32-bit rows), row_ld >= d,
+                                       0 <= head_ld <= 2^40, 0 <= page_ld <= 2^40             */
+  int32_t groups;     /* shared prefixes, 0..B (0: none, the fields below are ignored)        */
+  int32_t max_prefix; /* host-known upper bound of every prefix_len, 0..2^27                  */
+  const int32_t* group_cu;     /* DEVICE int32[groups+1] from 0 to B                          */
+  const int32_t* prefix_pages; /* DEVICE int32[groups][prefix_ld]                             */
+  const int32_t* prefix_len;   /* DEVICE int32[groups]                                        */
+  int32_t prefix_ld;           /* entries of a row of `prefix_pages`, >= 1                    */
+} dart_cache;
+
+/* Norms and rotates the heads of T tokens: head h of token t of q is the d elements from t*q_ld + h*d,
+ * of k from t*k_ld + h*d (so both may be views of a fused projection's rows); outputs likewise, and
+ * q_out may be q, k_out may be k.  Bases and strides are multiples of 16 bytes.
+ * pos: position ids, plane p of token t at pos[p*pos_plane_stride + t]; any value.
+ * l1_out (optional, float[T]): the L1 norm of every key row as it is stored (all Hkv heads, after
+ * rounding): the criterion norms that dart_reduce_with_norms takes with k_out as the criterion
+ * rows, good to 2^-20 of their value.                                                         */
+DART_API dart_status dart_norm_rotate(const dart_rotation* rotation, int32_t T, const void* q,
+                                      int64_t q_ld, const void* k, int64_t k_ld, const int64_t* pos,
+                                      int64_t pos_plane_stride, void* q_out, int64_t q_out_ld,
+                                      void* k_out, int64_t k_out_ld, float* l1_out, void* stream);
+
+/* The same for the tokens of `cache`, whose keys go to their pages, and with them the values (v, laid
+ * out like k, copied): token i of sequence b becomes key kv_len[b] - n_b + i, so kv_len[b] >= n_b is
+ * required.  k_out is optional here (rows of the keys beside the pages); k_out_ld is ignored without it.
+ * The queries of tokens that are not appended are written all the same.  Pages that two tokens of
+ * a call name as the same row get either's.                                                   */
+DART_API dart_status dart_norm_rotate_append(const dart_rotation* rotation, const dart_cache* cache,
+                                             const void* q, int64_t q_ld, const void* k, int64_t k_ld,
+                                             const void* v, int64_t v_ld, const int64_t* pos,
+                                             int64_t pos_plane_stride, void* q_out, int64_t q_out_ld,
+                                             void* k_out, int64_t k_out_ld, float* l1_out, void* k_pool,
+                                             void* v_pool, int32_t* status, void* stream);
+
+/* Bytes of workspace dart_attend needs for this descriptor (host arithmetic only; 0 if it is
+ * invalid). */
+DART_API size_t dart_attend_workspace_bytes(const dart_cache* cache);
+
+/* Attention over the cache.  Query head h of token t (d elements from t*q_ld + h*d, read with key head
+ * h / (Hq/Hkv)) sees its group's prefix and, of its sequence's own keys, those up to its own place:
+ * token i of sequence b sees keys j <= kv_len[b] - n_b + i with `causal`, all kv_len[b] without.  With
+ * s_j = scale * <q, k_j> and m the largest of them,
+ *   out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),   lse = m + ln sum_j exp(s_j - m);
+ * a token that sees nothing, or only scores of -infinity, gets zeros and -infinity.  out has the layout of q; lse (optional) is
+ * float[T][Hq].  Scores, sums and the running result are held in 32 bits; with bfloat16 rows the
+ * factors exp(s_j - m) are rounded to bfloat16 for the product with the values (and only there).
+ * A prefix is read once for all sequences of its group.  scale is finite. */
+DART_API dart_status dart_attend(const dart_cache* cache, const void* q, int64_t q_ld,
+                                 const void* k_pool, const void* v_pool, float scale, int32_t causal,
+                                 void* out, int64_t out_ld, float* lse, void* ws, size_t ws_bytes,
+                                 int32_t* status, void* stream);
+
 /* Static, NUL-terminated description of a status code. */
 DART_API const char* dart_strerror(dart_status status);
 

@@ -28,7 +28,9 @@ EXPORTS = ("dart_workspace_bytes", "dart_select_pivots", "dart_duplication_score
            "dart_reduce_profiled", "dart_reduce_static", "dart_static_scratch_bytes",
            "dart_device_status_static", "dart_probe_mfma_dot32", "dart_score_tile_shape",
            "dart_score_tile_shape_first_read", "dart_reduce_with_norms",
-           "dart_device_status", "dart_score_tolerance", "dart_strerror")
+           "dart_device_status", "dart_score_tolerance", "dart_norm_rotate",
+           "dart_norm_rotate_append", "dart_attend_workspace_bytes", "dart_attend",
+           "dart_strerror")
 
 
 class DartDesc(C.Structure):
@@ -46,6 +48,26 @@ class DartRowTensor(C.Structure):
     """Mirror of `struct dart_row_tensor`."""
     _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("row_bytes", C.c_int64),
                 ("src_ld_bytes", C.c_int64), ("dst_ld_bytes", C.c_int64)]
+
+
+class DartRotation(C.Structure):
+    """Mirror of `struct dart_rotation`."""
+    _fields_ = [("Hq", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int32),
+                ("rot", C.c_int32), ("interleaved", C.c_int32), ("planes", C.c_int32),
+                ("sections", C.c_int32 * 4), ("inv_freq", C.c_void_p), ("q_weight", C.c_void_p),
+                ("k_weight", C.c_void_p), ("eps", C.c_float), ("scale", C.c_float)]
+
+
+class DartCache(C.Structure):
+    """Mirror of `struct dart_cache`."""
+    _fields_ = [("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32),
+                ("dtype", C.c_int32), ("T", C.c_int32), ("max_q", C.c_int32),
+                ("max_kv", C.c_int32), ("cu_q", C.c_void_p), ("kv_len", C.c_void_p),
+                ("pages", C.c_void_p), ("pages_ld", C.c_int32), ("n_pages", C.c_int32),
+                ("page_size", C.c_int32), ("page_ld", C.c_int64), ("head_ld", C.c_int64),
+                ("row_ld", C.c_int64), ("groups", C.c_int32), ("max_prefix", C.c_int32),
+                ("group_cu", C.c_void_p), ("prefix_pages", C.c_void_p),
+                ("prefix_len", C.c_void_p), ("prefix_ld", C.c_int32)]
 
 
 class DartError(RuntimeError):
@@ -86,12 +108,20 @@ def lib():
         L.dart_static_scratch_bytes.restype = sz
         L.dart_device_status_static.argtypes = [dp, vp]
         L.dart_probe_mfma_dot32.argtypes = [vp, vp, vp, i32, vp]
+        rp, cp, f32 = C.POINTER(DartRotation), C.POINTER(DartCache), C.c_float
+        L.dart_norm_rotate.argtypes = [rp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]
+        L.dart_norm_rotate_append.argtypes = [rp, cp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64,
+                                              vp, i64, vp, vp, vp, vp, vp]
+        L.dart_attend_workspace_bytes.argtypes = [cp]
+        L.dart_attend_workspace_bytes.restype = sz
+        L.dart_attend.argtypes = [cp, vp, i64, vp, vp, f32, i32, vp, i64, vp, vp, sz, vp, vp]
         for name in ("dart_select_pivots", "dart_duplication_scores", "dart_topk_keep",
                      "dart_gather_compact", "dart_compact_sequences", "dart_reduce",
                      "dart_reduce_profiled", "dart_device_status", "dart_reduce_static",
                      "dart_device_status_static", "dart_probe_mfma_dot32",
                      "dart_score_tile_shape", "dart_score_tile_shape_first_read",
-                     "dart_reduce_with_norms"):
+                     "dart_reduce_with_norms", "dart_norm_rotate", "dart_norm_rotate_append",
+                     "dart_attend"):
             getattr(L, name).restype = C.c_int
         L.dart_score_tolerance.argtypes = [i32]
         L.dart_score_tolerance.restype = C.c_double
@@ -278,3 +308,164 @@ def dart_reduce_profiled(desc, X, Y, keep, ws, events, *, crit=None, crit_D=0, c
 
 def dart_device_status(desc, ws, *, stream=None) -> int:
     return int(lib().dart_device_status(C.byref(desc), _ptr(ws), _stream(stream)))
+
+
+# ---- attention on either side of the step ---------------------------------------------------
+
+_DTYPES = {torch.float32: DART_F32, torch.bfloat16: DART_BF16}
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _ints(t, what: str):
+    """An int32 device tensor whose last dimension is contiguous."""
+    _need(t.dtype == torch.int32 and (t.numel() == 0 or t.stride(-1) == 1), f"{what}: int32, contiguous rows")
+    return t
+
+
+def _rows(t, desc, heads: int, what: str):
+    """(address, row stride) of a tensor of rows [T, heads*d] or [T, heads, d] with contiguous
+    rows, such as a slice of a fused projection's output."""
+    if t.dim() == 3:
+        _need(t.shape[1:] == (heads, desc.d) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == desc.d),
+              f"{what}: [T, {heads}, {desc.d}] with contiguous rows")
+    else:
+        _need(t.dim() == 2 and t.shape[1] == heads * desc.d and t.stride(1) == 1,
+              f"{what}: [T, {heads * desc.d}] with contiguous rows")
+    _need(_DTYPES.get(t.dtype) == desc.dtype, f"{what}: dtype differs from the descriptor's")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else heads * desc.d)
+
+
+def make_rotation(Hq: int, Hkv: int, d: int, dtype: int, inv_freq: torch.Tensor, *,
+                  interleaved: bool = False, sections=None,
+                  q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                  eps: float = 1e-6, scale: float = 1.0) -> DartRotation:
+    """inv_freq: float32 [rot/2] on the device.  sections: pairs that follow each plane of position
+    ids, or None for one plane."""
+    r = DartRotation()
+    sections = [inv_freq.numel()] if sections is None else list(sections)
+    _need(inv_freq.dtype == torch.float32 and inv_freq.is_contiguous(), "inv_freq: contiguous float32")
+    _need(1 <= len(sections) <= 4 and sum(sections) == inv_freq.numel(), "sections: up to 4, summing to the pairs")
+    for w in (q_weight, k_weight):
+        _need(w is None or (w.numel() == d and w.is_contiguous() and _DTYPES.get(w.dtype) == dtype),
+              "weights: contiguous [d] of the rows' dtype")
+    r.Hq, r.Hkv, r.d, r.dtype = Hq, Hkv, d, dtype
+    r.rot, r.interleaved, r.planes = 2 * inv_freq.numel(), int(interleaved), len(sections)
+    r.sections[:len(sections)] = sections
+    r.inv_freq = inv_freq.data_ptr()
+    r.q_weight = None if q_weight is None else q_weight.data_ptr()
+    r.k_weight = None if k_weight is None else k_weight.data_ptr()
+    r.eps, r.scale = eps, scale
+    r._keepalive = (inv_freq, q_weight, k_weight)
+    return r
+
+
+def make_cache(Hq: int, pool: torch.Tensor, pages: torch.Tensor, kv_len: torch.Tensor, max_kv: int, *,
+               T: Optional[int] = None, max_q: int = 1, cu_q: Optional[torch.Tensor] = None,
+               group_cu: Optional[torch.Tensor] = None, prefix_pages: Optional[torch.Tensor] = None,
+               prefix_len: Optional[torch.Tensor] = None, max_prefix: int = 0) -> DartCache:
+    """pool: the key pool [pages, Hkv, page_size, d], any strides with contiguous heads (so a pool
+    whose memory holds [pages, page_size, Hkv, d] is passed transposed); the value pool is laid out
+    like it.  pages: int32 [B, n]; kv_len: int32 [B] with the tokens of the call.  cu_q: int32 [B+1] and T
+    tokens, at most max_q of a sequence; without it one token each."""
+    _need(pool.dim() == 4 and pool.stride(3) == 1 and pool.dtype in _DTYPES, "pool: [pages, Hkv, page_size, d]")
+    _need(pages.dim() == 2 and kv_len.numel() == pages.shape[0], "pages: [B, n], kv_len: [B]")
+    c = DartCache()
+    c.B, c.Hq, c.Hkv, c.d, c.dtype = pages.shape[0], Hq, pool.shape[1], pool.shape[3], _DTYPES[pool.dtype]
+    _need(cu_q is None or (T is not None and cu_q.numel() == c.B + 1), "cu_q: [B+1], with T")
+    c.T, c.max_q, c.max_kv = (c.B if T is None else T), max_q, max_kv
+    c.cu_q = None if cu_q is None else _ints(cu_q, "cu_q").data_ptr()
+    c.kv_len, c.pages = _ints(kv_len, "kv_len").data_ptr(), _ints(pages, "pages").data_ptr()
+    c.pages_ld = pages.stride(0) if c.B > 1 else pages.shape[1]
+    c.n_pages, c.page_size = pool.shape[0], pool.shape[2]
+    c.row_ld = pool.stride(2) if c.page_size > 1 else c.d
+    c.head_ld = pool.stride(1) if c.Hkv > 1 else 0
+    c.page_ld = pool.stride(0) if c.n_pages > 1 else 0
+    if group_cu is not None:
+        c.groups = prefix_len.numel()
+        _need(group_cu.numel() == c.groups + 1 and prefix_pages.dim() == 2 and prefix_pages.shape[0] == c.groups,
+              "group_cu: [groups+1], prefix_pages: [groups, n], prefix_len: [groups]")
+        c.group_cu, c.prefix_len = _ints(group_cu, "group_cu").data_ptr(), _ints(prefix_len, "prefix_len").data_ptr()
+        c.prefix_pages = _ints(prefix_pages, "prefix_pages").data_ptr()
+        c.prefix_ld = prefix_pages.stride(0) if c.groups > 1 else prefix_pages.shape[1]
+        c.max_prefix = max_prefix
+    c._keepalive = (pages, kv_len, cu_q, group_cu, prefix_pages, prefix_len)
+    return c
+
+
+def _pools(cache: DartCache, k_pool, v_pool):
+    for p in (k_pool, v_pool):
+        _need(p.shape == (cache.n_pages, cache.Hkv, cache.page_size, cache.d) and _DTYPES.get(p.dtype) == cache.dtype
+              and (cache.page_size == 1 or p.stride(2) == cache.row_ld)
+              and (cache.Hkv == 1 or p.stride(1) == cache.head_ld)
+              and (cache.n_pages == 1 or p.stride(0) == cache.page_ld) and p.stride(3) == 1,
+              "pools: shape, strides and dtype of the pool the descriptor was made for")
+    return k_pool.data_ptr(), v_pool.data_ptr()
+
+
+def _planes(pos, planes: int, T: int):
+    """(address, plane stride) of position ids [T] or [planes, T], int64."""
+    _need(pos.dtype == torch.int64 and pos.stride(-1) == 1 and pos.numel() == planes * T and pos.shape[-1] == T,
+          "pos: int64 [planes, T]")
+    return pos.data_ptr(), (pos.stride(0) if planes > 1 else 0)
+
+
+def dart_norm_rotate(rotation: DartRotation, q, k, pos, q_out, k_out, *, l1_out=None, stream=None):
+    """Heads of q [T, Hq*d] and k [T, Hkv*d] normed and turned by their position ids (int64 [T] or
+    [planes, T]) into q_out and k_out (which may be q and k); l1_out float32 [T]: the L1 norms
+    of the key rows."""
+    T = q.shape[0]
+    _need(k.shape[0] == T and q_out.shape[0] == T and k_out.shape[0] == T, "rows: T of each")
+    _need(l1_out is None or (l1_out.numel() == T and l1_out.dtype == torch.float32), "l1_out: float32 [T]")
+    if T == 0:
+        return
+    r = rotation
+    _check(lib().dart_norm_rotate(C.byref(r), T, *_rows(q, r, r.Hq, "q"), *_rows(k, r, r.Hkv, "k"),
+                                  *_planes(pos, r.planes, T), *_rows(q_out, r, r.Hq, "q_out"),
+                                  *_rows(k_out, r, r.Hkv, "k_out"), _ptr(l1_out), _stream(stream)),
+           "dart_norm_rotate")
+
+
+def dart_norm_rotate_append(rotation: DartRotation, cache: DartCache, q, k, v, pos, q_out, k_pool, v_pool, *,
+                            k_out=None, l1_out=None, status=None, stream=None):
+    """dart_norm_rotate for the tokens of `cache`, keys and values going to their pages.  status:
+    int32 [1] that bits are OR-ed into, or None."""
+    T, r = cache.T, rotation
+    _need(all(x is None or x.shape[0] == T for x in (q, k, v, q_out, k_out)), "rows: T of each")
+    _need(l1_out is None or (l1_out.numel() == T and l1_out.dtype == torch.float32), "l1_out: float32 [T]")
+    if T == 0:
+        return
+    ko = (None, 0) if k_out is None else _rows(k_out, r, r.Hkv, "k_out")
+    _check(lib().dart_norm_rotate_append(
+        C.byref(r), C.byref(cache), *_rows(q, r, r.Hq, "q"), *_rows(k, r, r.Hkv, "k"), *_rows(v, r, r.Hkv, "v"),
+        *_planes(pos, r.planes, T), *_rows(q_out, r, r.Hq, "q_out"), *ko, _ptr(l1_out),
+        *_pools(cache, k_pool, v_pool), _ptr(status), _stream(stream)), "dart_norm_rotate_append")
+
+
+def dart_attend_workspace_bytes(cache: DartCache) -> int:
+    return int(lib().dart_attend_workspace_bytes(C.byref(cache)))
+
+
+def alloc_attend_workspace(cache: DartCache, device="cuda") -> torch.Tensor:
+    n = dart_attend_workspace_bytes(cache)
+    if n == 0:
+        raise DartError(DART_ERR_SHAPE, "dart_attend_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def dart_attend(cache: DartCache, q, k_pool, v_pool, out, ws, *, scale: float, causal: bool = True, lse=None,
+                status=None, stream=None):
+    """Attention of the tokens' queries q [T, Hq*d] over the cache (and the shared prefixes) into
+    out [T, Hq*d]; lse float32 [T, Hq]."""
+    T, c = cache.T, cache
+    _need(q.shape[0] == T and out.shape[0] == T, "rows: T of each")
+    _need(lse is None or (lse.numel() == T * c.Hq and lse.dtype == torch.float32 and lse.is_contiguous()),
+          "lse: float32 [T, Hq]")
+    if T == 0:
+        return
+    _check(lib().dart_attend(C.byref(c), *_rows(q, c, c.Hq, "q"), *_pools(c, k_pool, v_pool), scale, int(causal),
+                             *_rows(out, c, c.Hq, "out"), _ptr(lse), _ptr(ws), ws.numel(), _ptr(status),
+                             _stream(stream)), "dart_attend")

@@ -12,10 +12,13 @@ import glob
 import hashlib
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
+SOURCES = ("dart_api.hip", "attend_api.hip")  # translation units, compiled side by side
 LIB = os.path.join(_HERE, "libdart_hip.so")  # the path binding.py loads
 STAMP = LIB + ".sha256"
 
@@ -40,17 +43,33 @@ def source_hash() -> str:
     return h.hexdigest()
 
 
-def build_hip(verbose: bool = False) -> str:
+def _compile(flags, out: str) -> str:
+    """Compiles the translation units with these flags (without -shared) and links them to `out`;
+    returns what the compiler said."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    src = os.path.join(CSRC, "dart_api.hip")
-    cmd = [hipcc, *HIPCC_FLAGS, src, "-o", LIB]
+    said = []
+
+    def hip(cmd):
+        res = subprocess.run([hipcc, *cmd], capture_output=True, text=True)
+        noise = "is not a recognized feature for this target"
+        err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
+        if res.returncode != 0:
+            raise RuntimeError(f"hipcc failed ({res.returncode}):\n{err}")
+        said.append(err)
+
+    with tempfile.TemporaryDirectory() as td, ThreadPoolExecutor(len(SOURCES)) as pool:
+        objs = [os.path.join(td, src + ".o") for src in SOURCES]
+        list(pool.map(lambda so: hip([*flags, "-c", os.path.join(CSRC, so[0]), "-o", so[1]]),
+                      zip(SOURCES, objs)))
+        hip([*flags, "-shared", *objs, "-o", out])
+    return "\n".join(e for e in said if e.strip())
+
+
+def build_hip(verbose: bool = False) -> str:
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"]
     if verbose:
-        print(" ".join(cmd))
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    noise = "is not a recognized feature for this target"
-    err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
-    if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{err}")
+        print("hipcc", *flags, *SOURCES, "->", LIB)
+    err = _compile(flags, LIB)
     if verbose and err.strip():
         print(err)
     with open(STAMP, "w") as f:
@@ -72,14 +91,10 @@ def build_host_sanitized(outdir: str) -> str:
                 return out
     except OSError:
         pass
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    flags = [f for f in HIPCC_FLAGS if f != "-O3"] + ["-O1", "-g"]
+    flags = [f for f in HIPCC_FLAGS if f not in ("-O3", "-shared")] + ["-O1", "-g"]
     for san in ("-fsanitize=address", "-fsanitize=undefined", "-fno-sanitize-recover=all"):
         flags += ["-Xarch_host", san]
-    res = subprocess.run([hipcc, *flags, os.path.join(CSRC, "dart_api.hip"), "-o", out],
-                         capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError(f"hipcc (host sanitizers) failed ({res.returncode}):\n{res.stderr}")
+    _compile(flags, out)
     with open(stamp, "w") as f:
         f.write(source_hash() + "\n")
     return out

@@ -1,0 +1,239 @@
+// Host side of the attention calls of include/dart.h: argument checks, the choice of variants
+// and kernel launches.  No allocation, no synchronisation.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/dart.h"
+#include "cache.hpp"
+#include "k_attend.hpp"
+#include "k_rotate.hpp"
+
+using namespace dart;
+
+namespace {
+
+constexpr size_t kAlign = 256;
+constexpr int64_t kMaxLd = int64_t(1) << 24;       // row strides of q, k, v and outputs, elements
+constexpr int64_t kMaxPoolLd = int64_t(1) << 40;   // strides inside the pools, elements
+constexpr int kMaxSequences = 1 << 20, kMaxTokens = 1 << 24, kMaxKeys = 1 << 27, kMaxPage = 1 << 20;
+constexpr int kMaxHeads = 1024, kMaxHead = 256;
+
+inline bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+inline int elem(int dtype) { return dtype == DART_BF16 ? 2 : 4; }
+
+#define DART_TRY(expr)                    \
+  do {                                    \
+    dart_status _s = (expr);              \
+    if (_s != DART_OK) return _s;         \
+  } while (0)
+
+dart_status launched() { return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP; }
+
+dart_status check_heads(int Hq, int Hkv, int d, int dtype) {
+  if (dtype != DART_F32 && dtype != DART_BF16) return DART_ERR_DTYPE;
+  if (Hkv < 1 || Hq < Hkv || Hq > kMaxHeads || Hq % Hkv || d < 8 || d > kMaxHead || d % 8) return DART_ERR_SHAPE;
+  return DART_OK;
+}
+
+// A tensor of rows of `width` elements.
+dart_status check_rows(const void* p, int64_t ld, int64_t width, int dtype) {
+  if (!p) return DART_ERR_NULL;
+  if (ld < width || ld > kMaxLd) return DART_ERR_SHAPE;
+  if (off16(p) || ld * elem(dtype) % 16) return DART_ERR_ALIGN;
+  return DART_OK;
+}
+
+dart_status make_cache(const dart_cache* u, Cache& c) {
+  if (!u) return DART_ERR_NULL;
+  DART_TRY(check_heads(u->Hq, u->Hkv, u->d, u->dtype));
+  if (u->B < 0 || u->B > kMaxSequences || u->T < 0 || u->T > kMaxTokens || u->max_q < 0 || u->max_kv < 0 ||
+      u->max_kv > kMaxKeys || u->pages_ld < 1 || u->n_pages < 1)
+    return DART_ERR_SHAPE;
+  if (u->page_size < 1 || u->page_size > kMaxPage || (u->page_size & (u->page_size - 1))) return DART_ERR_SHAPE;
+  if (u->row_ld < u->d || u->row_ld > kMaxPoolLd || u->head_ld < 0 || u->head_ld > kMaxPoolLd || u->page_ld < 0 ||
+      u->page_ld > kMaxPoolLd)
+    return DART_ERR_SHAPE;
+  if (u->groups < 0 || u->groups > u->B) return DART_ERR_SHAPE;
+  if (!u->cu_q && u->T != u->B) return DART_ERR_SHAPE;
+  const int64_t a16 = 16 / elem(u->dtype);
+  if (u->row_ld % a16 || u->head_ld % a16 || u->page_ld % a16) return DART_ERR_ALIGN;
+  c = {};
+  c.B = u->B;
+  c.Hq = u->Hq;
+  c.Hkv = u->Hkv;
+  c.d = u->d;
+  c.T = u->T;
+  c.max_q = u->cu_q ? std::min(u->max_q, u->T) : 1;
+  c.max_kv = u->max_kv;
+  c.cu = u->cu_q;
+  c.kv_len = u->kv_len;
+  c.pages = u->pages;
+  c.pages_ld = u->pages_ld;
+  c.n_pages = u->n_pages;
+  c.page_shift = __builtin_ctz((unsigned)u->page_size);
+  c.page_ld = u->page_ld;
+  c.head_ld = u->head_ld;
+  c.row_ld = u->row_ld;
+  c.groups = u->groups;
+  if (u->groups > 0) {
+    if (u->max_prefix < 0 || u->max_prefix > kMaxKeys || u->prefix_ld < 1) return DART_ERR_SHAPE;
+    if (!u->group_cu || !u->prefix_pages || !u->prefix_len) return DART_ERR_NULL;
+    c.max_prefix = u->max_prefix;
+    c.prefix_ld = u->prefix_ld;
+    c.group_cu = u->group_cu;
+    c.prefix_pages = u->prefix_pages;
+    c.prefix_len = u->prefix_len;
+  }
+  if (u->B > 0 && (!u->kv_len || !u->pages)) return DART_ERR_NULL;
+  return DART_OK;
+}
+
+dart_status make_rotate(const dart_rotation* u, Rotate& a) {
+  if (!u) return DART_ERR_NULL;
+  DART_TRY(check_heads(u->Hq, u->Hkv, u->d, u->dtype));
+  if (u->rot < 0 || u->rot > u->d || u->rot % 8 || u->planes < 1 || u->planes > kMaxPlanes) return DART_ERR_SHAPE;
+  if (!(u->eps >= 0.f) || !std::isfinite(u->eps) || !std::isfinite(u->scale)) return DART_ERR_SHAPE;
+  if (u->rot > 0 && !u->inv_freq) return DART_ERR_NULL;
+  if ((u->q_weight && off16(u->q_weight)) || (u->k_weight && off16(u->k_weight))) return DART_ERR_ALIGN;
+  a = {};
+  a.Hq = u->Hq;
+  a.Hkv = u->Hkv;
+  a.d = u->d;
+  a.half = u->rot / 2;
+  a.interleaved = u->interleaved != 0;
+  a.planes = u->planes;
+  int end = 0;
+  for (int p = 0; p < kMaxPlanes; ++p) {
+    if (u->planes > 1 && p < u->planes) {
+      if (u->sections[p] < 0 || u->sections[p] > a.half - end) return DART_ERR_SHAPE;
+      end += u->sections[p];
+    }
+    a.section_end[p] = u->planes > 1 ? end : a.half;
+  }
+  if (u->planes > 1 && end != a.half) return DART_ERR_SHAPE;
+  a.inv_freq = u->inv_freq;
+  a.qw = u->q_weight;
+  a.kw = u->k_weight;
+  a.eps = u->eps;
+  a.scale = u->scale;
+  return DART_OK;
+}
+
+template <int DT, int VE, bool APPEND>
+dart_status launch_rotate(Rotate& a, const Cache& c, hipStream_t st) {
+  const int rest = a.d - 2 * a.half;
+  a.units = a.half / VE + (rest + 2 * VE - 1) / (2 * VE);
+  a.lanes_shift = 0;
+  while ((1 << a.lanes_shift) < a.units) ++a.lanes_shift;
+  if (a.T < 4096)
+    k_norm_rotate<DT, VE, 4, APPEND><<<dim3(a.T), dim3(256), 0, st>>>(a, c);
+  else
+    k_norm_rotate<DT, VE, 1, APPEND><<<dim3((a.T + 3) / 4), dim3(256), 0, st>>>(a, c);
+  return launched();
+}
+
+template <bool APPEND>
+dart_status rotate(Rotate& a, const Cache& c, int dtype, hipStream_t st) {
+  if (dtype == DART_F32) return launch_rotate<kF32, 4, APPEND>(a, c, st);
+  // pieces of 16 bytes unless a pair's two elements would then not fall to one lane
+  return a.half % 8 == 0 ? launch_rotate<kBF16, 8, APPEND>(a, c, st) : launch_rotate<kBF16, 4, APPEND>(a, c, st);
+}
+
+dart_status set_rows(Rotate& a, int dtype, int T, const void* q, int64_t q_ld, const void* k, int64_t k_ld,
+                     const int64_t* pos, int64_t pos_ld, void* q_out, int64_t q_out_ld, void* k_out, int64_t k_out_ld,
+                     float* l1) {
+  if (!pos) return DART_ERR_NULL;
+  if (a.planes > 1 && pos_ld < T) return DART_ERR_SHAPE;
+  DART_TRY(check_rows(q, q_ld, (int64_t)a.Hq * a.d, dtype));
+  DART_TRY(check_rows(k, k_ld, (int64_t)a.Hkv * a.d, dtype));
+  DART_TRY(check_rows(q_out, q_out_ld, (int64_t)a.Hq * a.d, dtype));
+  if (k_out) DART_TRY(check_rows(k_out, k_out_ld, (int64_t)a.Hkv * a.d, dtype));
+  a.T = T;
+  a.q = q;
+  a.k = k;
+  a.q_ld = q_ld;
+  a.k_ld = k_ld;
+  a.pos = reinterpret_cast<const long long*>(pos);
+  a.pos_ld = a.planes > 1 ? pos_ld : 0;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.q_out_ld = q_out_ld;
+  a.k_out_ld = k_out_ld;
+  a.l1 = l1;
+  return DART_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+dart_status dart_norm_rotate(const dart_rotation* rotation, int32_t T, const void* q, int64_t q_ld, const void* k,
+                             int64_t k_ld, const int64_t* pos, int64_t pos_plane_stride, void* q_out, int64_t q_out_ld,
+                             void* k_out, int64_t k_out_ld, float* l1_out, void* stream) {
+  Rotate a;
+  DART_TRY(make_rotate(rotation, a));
+  if (T < 0 || T > kMaxTokens) return DART_ERR_SHAPE;
+  if (T == 0) return DART_OK;
+  if (!k_out) return DART_ERR_NULL;
+  DART_TRY(set_rows(a, rotation->dtype, T, q, q_ld, k, k_ld, pos, pos_plane_stride, q_out, q_out_ld, k_out, k_out_ld,
+                    l1_out));
+  return rotate<false>(a, Cache{}, rotation->dtype, static_cast<hipStream_t>(stream));
+}
+
+dart_status dart_norm_rotate_append(const dart_rotation* rotation, const dart_cache* cache, const void* q,
+                                    int64_t q_ld, const void* k, int64_t k_ld, const void* v, int64_t v_ld,
+                                    const int64_t* pos, int64_t pos_plane_stride, void* q_out, int64_t q_out_ld,
+                                    void* k_out, int64_t k_out_ld, float* l1_out, void* k_pool, void* v_pool,
+                                    int32_t* status, void* stream) {
+  Rotate a;
+  Cache c;
+  DART_TRY(make_rotate(rotation, a));
+  DART_TRY(make_cache(cache, c));
+  if (rotation->dtype != cache->dtype) return DART_ERR_DTYPE;
+  if (a.Hq != c.Hq || a.Hkv != c.Hkv || a.d != c.d) return DART_ERR_SHAPE;
+  if (c.T == 0 || c.B == 0) return DART_OK;
+  DART_TRY(set_rows(a, rotation->dtype, c.T, q, q_ld, k, k_ld, pos, pos_plane_stride, q_out, q_out_ld, k_out, k_out_ld,
+                    l1_out));
+  DART_TRY(check_rows(v, v_ld, (int64_t)a.Hkv * a.d, cache->dtype));
+  if (!k_pool || !v_pool) return DART_ERR_NULL;
+  if (off16(k_pool) || off16(v_pool)) return DART_ERR_ALIGN;
+  a.v = v;
+  a.v_ld = v_ld;
+  a.k_pool = k_pool;
+  a.v_pool = v_pool;
+  c.status = status;
+  return rotate<true>(a, c, cache->dtype, static_cast<hipStream_t>(stream));
+}
+
+size_t dart_attend_workspace_bytes(const dart_cache* cache) {
+  Cache c;
+  if (make_cache(cache, c) != DART_OK) return 0;
+  return kAlign;
+}
+
+dart_status dart_attend(const dart_cache* cache, const void* q, int64_t q_ld, const void* k_pool, const void* v_pool,
+                        float scale, int32_t causal, void* out, int64_t out_ld, float* lse, void* ws, size_t ws_bytes,
+                        int32_t* status, void* stream) {
+  Cache c;
+  DART_TRY(make_cache(cache, c));
+  if (!std::isfinite(scale)) return DART_ERR_SHAPE;
+  if (c.T == 0 || c.B == 0) return DART_OK;
+  DART_TRY(check_rows(q, q_ld, (int64_t)c.Hq * c.d, cache->dtype));
+  DART_TRY(check_rows(out, out_ld, (int64_t)c.Hq * c.d, cache->dtype));
+  if (!k_pool || !v_pool) return DART_ERR_NULL;
+  if (off16(k_pool) || off16(v_pool)) return DART_ERR_ALIGN;
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < dart_attend_workspace_bytes(cache))
+    return DART_ERR_WORKSPACE;
+  c.status = status;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const Attend a = {q, k_pool, v_pool, out, lse, q_ld, out_ld, scale, causal != 0};
+  if (cache->dtype == DART_BF16)
+    k_attend_rows<kBF16><<<dim3(c.T, c.Hq), dim3(64), 0, st>>>(a, c);
+  else
+    k_attend_rows<kF32><<<dim3(c.T, c.Hq), dim3(64), 0, st>>>(a, c);
+  return launched();
+}
+
+}  // extern "C"

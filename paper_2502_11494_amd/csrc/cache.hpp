@@ -1,0 +1,80 @@
+// The paged cache as kernels see it, and the checks every one of them makes the same way.
+#pragma once
+
+#include "common.hpp"
+
+namespace dart {
+
+enum { kBadSequence = 1, kBadPage = 2 };  // bits of the caller's status word
+
+struct Cache {
+  int B, Hq, Hkv, d, T, max_q, max_kv;
+  const int *cu, *kv_len, *pages;
+  int pages_ld, n_pages, page_shift;
+  long page_ld, head_ld, row_ld;  // elements
+  int groups, max_prefix, prefix_ld;
+  const int *group_cu, *prefix_pages, *prefix_len;
+  int* status;
+};
+
+__device__ __forceinline__ void flag(const Cache& c, int bit) {
+  if (c.status != nullptr) atomicOr(c.status, bit);
+}
+
+// The last of count offsets that is at most v, 0 if none is: last_at_most for offsets that nothing has
+// checked yet (any index it gives is one of theirs).
+__device__ __forceinline__ int owner_of(const int* offset, int count, int v) {
+  const int lane = threadIdx.x & 63;
+  int from = 0, left = count;
+  while (true) {
+    const int stride = (left + kWave - 1) / kWave, d = lane * stride;
+    const unsigned long long low = __ballot(d < left && offset[from + (d < left ? d : 0)] <= v);
+    const int skip = (low ? 63 - __builtin_clzll(low) : 0) * stride;
+    from += skip;
+    if (stride == 1) return __builtin_amdgcn_readfirstlane(from);
+    left = left - skip < stride ? left - skip : stride;
+  }
+}
+
+// The tokens and keys of one sequence; valid: its offsets and lengths are as they have to be.  Of a
+// sequence that is not, [tok0, tok0 + n) are those of its tokens that are tokens of the call.
+struct Seq {
+  int tok0, n, kv;
+  bool valid;
+};
+
+__device__ __forceinline__ Seq sequence_of(const Cache& c, int b) {
+  Seq s;
+  if (c.cu == nullptr) {
+    s.tok0 = b;
+    s.n = 1;
+    s.valid = true;
+  } else {
+    const int lo = c.cu[b], hi = c.cu[b + 1];
+    s.valid = lo >= 0 && hi >= lo && hi <= c.T && hi - lo <= c.max_q;
+    s.tok0 = lo < 0 ? 0 : lo < c.T ? lo : c.T;
+    s.n = (hi < c.T ? hi : c.T) - s.tok0;
+    if (s.n < 0) s.n = 0;
+  }
+  s.kv = c.kv_len[b];
+  if (s.kv < 0 || s.kv > c.max_kv || (long)s.kv > ((long)c.pages_ld << c.page_shift)) s.valid = false;
+  if (!s.valid) s.kv = 0;
+  return s;
+}
+
+// Keys of group g's prefix; -1 if its length or its sequences are not as they have to be.
+__device__ __forceinline__ int prefix_of(const Cache& c, int g) {
+  const int n = c.prefix_len[g], b0 = c.group_cu[g], b1 = c.group_cu[g + 1];
+  if (n < 0 || n > c.max_prefix || (long)n > ((long)c.prefix_ld << c.page_shift) || b0 < 0 || b1 < b0 || b1 > c.B)
+    return -1;
+  return n;
+}
+
+// The offset of row `key` of a page table's keys, in elements; of page 0 if its page is none.
+__device__ __forceinline__ long key_offset(const Cache& c, const int* table, int key, bool& bad) {
+  const int page = table[key >> c.page_shift];
+  bad = (unsigned)page >= (unsigned)c.n_pages;
+  return (bad ? 0L : (long)page * c.page_ld) + (long)(key & ((1 << c.page_shift) - 1)) * c.row_ld;
+}
+
+}  // namespace dart
