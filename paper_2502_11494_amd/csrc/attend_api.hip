@@ -19,6 +19,7 @@ constexpr int64_t kMaxLd = int64_t(1) << 24;       // row strides of q, k, v and
 constexpr int64_t kMaxPoolLd = int64_t(1) << 40;   // strides inside the pools, elements
 constexpr int kMaxSequences = 1 << 20, kMaxTokens = 1 << 24, kMaxKeys = 1 << 27, kMaxPage = 1 << 20;
 constexpr int kMaxHeads = 1024, kMaxHead = 256;
+constexpr long kMaxSlots = (1 << 23) - 1;          // row tiles of one launch
 
 inline bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 inline int elem(int dtype) { return dtype == DART_BF16 ? 2 : 4; }
@@ -165,6 +166,90 @@ dart_status set_rows(Rotate& a, int dtype, int T, const void* q, int64_t q_ld, c
   return DART_OK;
 }
 
+// ---- attention: which tiles, how many parts ---------------------------------------------------
+enum Kind { kFew, kMany, kWide };  // 32 rows, the keys dealt to four waves; 128 rows; 256 rows
+
+struct Launch {
+  Kind kind;
+  int bm, chunk, chunks;
+  long slots;
+};
+
+struct AttendPlan {
+  Launch own, pre;
+  int parts;
+  size_t o_o, o_ml, total;
+};
+
+int rows_of(Kind k) { return k == kFew ? 32 : k == kMany ? 128 : 256; }
+
+// rows: (token, head) pairs of a sequence or group at most; owners: how many of them.
+Launch plan_launch(const Cache& c, int dtype, long rows, int owners, int max_keys) {
+  Launch l;
+  const int r = c.Hq / c.Hkv;
+  l.kind = rows <= 32 ? kFew : rows <= 128 || dtype == DART_F32 || c.d > 128 ? kMany : kWide;
+  if (dtype == DART_F32 && c.d > 128) l.kind = kMany;
+  l.bm = rows_of(l.kind);
+  l.slots = (long)c.T * r / l.bm + owners;
+  const long blocks = std::max(1L, std::min(l.slots, (long)owners * ((rows + l.bm - 1) / l.bm)) * c.Hkv);
+  // enough parts to fill the chip twice, of 256 keys at least
+  const long want = std::max(1L, 512 / blocks);
+  long chunk = (max_keys + want - 1) / want;
+  chunk = std::max(256L, (chunk + 255) / 256 * 256);
+  l.chunk = (int)chunk;
+  l.chunks = std::max(1, (int)((max_keys + chunk - 1) / chunk));
+  return l;
+}
+
+dart_status plan_attend(const Cache& c, int dtype, AttendPlan& p) {
+  const int r = c.Hq / c.Hkv;
+  p = {};
+  p.own = plan_launch(c, dtype, (long)c.max_q * r, c.B, c.max_kv);
+  p.parts = p.own.chunks;
+  if (c.groups > 0) {
+    const long rows = std::min((long)c.T, (long)c.max_q * c.B) * r;
+    p.pre = plan_launch(c, dtype, std::max(1L, (rows + c.groups - 1) / c.groups), c.groups, c.max_prefix);
+    p.parts += p.pre.chunks;
+  }
+  if (p.own.slots > kMaxSlots || p.pre.slots > kMaxSlots || p.parts > 65535) return DART_ERR_SHAPE;
+  auto up = [](size_t v) { return (v + kAlign - 1) / kAlign * kAlign; };
+  const size_t rows = (size_t)c.T * c.Hq;
+  p.total = kAlign;
+  if (p.parts > 1) {
+    p.o_ml = up((size_t)p.parts * rows * c.d * 4);
+    p.total = p.o_ml + up((size_t)p.parts * rows * 8);
+  }
+  return DART_OK;
+}
+
+template <int DT, int DP, int WM, int WK, int QT, int KT>
+dart_status launch_tiles(const Attend& a, const Cache& c, const Parting& sp, const Launch& l, hipStream_t st) {
+  typedef AttendShape<DT, DP, WM, WK, QT, KT> S;
+  k_attend<DT, DP, WM, WK, QT, KT><<<dim3((unsigned)l.slots, c.Hkv, l.chunks), dim3(S::kThreads), S::kLds, st>>>(a, c, sp);
+  return launched();
+}
+
+template <int DP>
+dart_status launch_bf16(const Attend& a, const Cache& c, const Parting& sp, const Launch& l, hipStream_t st) {
+  if (l.kind == kFew) return launch_tiles<kBF16, DP, 1, 4, 1, 32>(a, c, sp, l, st);
+  if constexpr (DP <= 128)
+    if (l.kind == kWide) return launch_tiles<kBF16, DP, 4, 1, 2, 64>(a, c, sp, l, st);
+  return launch_tiles<kBF16, DP, 4, 1, 1, 64>(a, c, sp, l, st);
+}
+
+template <int DP>
+dart_status launch_f32(const Attend& a, const Cache& c, const Parting& sp, const Launch& l, hipStream_t st) {
+  if constexpr (DP <= 128)
+    if (l.kind == kFew) return launch_tiles<kF32, DP, 1, 4, 1, 32>(a, c, sp, l, st);
+  return launch_tiles<kF32, DP, 4, 1, 1, 32>(a, c, sp, l, st);
+}
+
+dart_status launch_attend(const Attend& a, const Cache& c, int dtype, const Parting& sp, const Launch& l, hipStream_t st) {
+  if (dtype == DART_BF16)
+    return c.d <= 64 ? launch_bf16<64>(a, c, sp, l, st) : c.d <= 128 ? launch_bf16<128>(a, c, sp, l, st) : launch_bf16<256>(a, c, sp, l, st);
+  return c.d <= 64 ? launch_f32<64>(a, c, sp, l, st) : c.d <= 128 ? launch_f32<128>(a, c, sp, l, st) : launch_f32<256>(a, c, sp, l, st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -209,8 +294,9 @@ dart_status dart_norm_rotate_append(const dart_rotation* rotation, const dart_ca
 
 size_t dart_attend_workspace_bytes(const dart_cache* cache) {
   Cache c;
-  if (make_cache(cache, c) != DART_OK) return 0;
-  return kAlign;
+  AttendPlan p;
+  if (make_cache(cache, c) != DART_OK || plan_attend(c, cache->dtype, p) != DART_OK) return 0;
+  return p.total;
 }
 
 dart_status dart_attend(const dart_cache* cache, const void* q, int64_t q_ld, const void* k_pool, const void* v_pool,
@@ -224,15 +310,26 @@ dart_status dart_attend(const dart_cache* cache, const void* q, int64_t q_ld, co
   DART_TRY(check_rows(out, out_ld, (int64_t)c.Hq * c.d, cache->dtype));
   if (!k_pool || !v_pool) return DART_ERR_NULL;
   if (off16(k_pool) || off16(v_pool)) return DART_ERR_ALIGN;
-  if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < dart_attend_workspace_bytes(cache))
-    return DART_ERR_WORKSPACE;
+  AttendPlan p;
+  DART_TRY(plan_attend(c, cache->dtype, p));
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < p.total) return DART_ERR_WORKSPACE;
   c.status = status;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const Attend a = {q, k_pool, v_pool, out, lse, q_ld, out_ld, scale, causal != 0};
+  float* part_o = static_cast<float*>(ws);
+  float2* part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(ws) + p.o_ml);
+  if (c.groups > 0) DART_TRY(launch_attend(a, c, cache->dtype, {1, p.pre.chunk, 0, p.parts, part_o, part_ml}, p.pre, st));
+  DART_TRY(launch_attend(a, c, cache->dtype, {0, p.own.chunk, p.pre.chunks, p.parts, part_o, part_ml}, p.own, st));
+  if (p.parts == 1) return DART_OK;
+  int lanes_shift = 0;
+  while ((4 << lanes_shift) < c.d) ++lanes_shift;
+  const long per_block = 4L << (6 - lanes_shift), blocks = ((long)c.T * c.Hq + per_block - 1) / per_block;
   if (cache->dtype == DART_BF16)
-    k_attend_rows<kBF16><<<dim3(c.T, c.Hq), dim3(64), 0, st>>>(a, c);
+    k_attend_join<kBF16><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, part_o, part_ml,
+                                                                      lanes_shift);
   else
-    k_attend_rows<kF32><<<dim3(c.T, c.Hq), dim3(64), 0, st>>>(a, c);
+    k_attend_join<kF32><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, part_o, part_ml,
+                                                                     lanes_shift);
   return launched();
 }
 
