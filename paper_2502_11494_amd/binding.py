@@ -143,8 +143,15 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
-def _stream(stream) -> C.c_void_p:
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(stream):
+    """The hipStream_t of a torch stream, of a raw handle, or of the current stream (asked for as a
+    handle: a stream object costs 3 us, as much as the launch it is for)."""
     if stream is None:
+        if _raw_stream is not None and torch.cuda.is_initialized():
+            return _raw_stream(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return C.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
@@ -313,30 +320,47 @@ def dart_device_status(desc, ws, *, stream=None) -> int:
 # ---- attention on either side of the step ---------------------------------------------------
 
 _DTYPES = {torch.float32: DART_F32, torch.bfloat16: DART_BF16}
+_KINDS = {v: k for k, v in _DTYPES.items()}
 
-
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
+# These calls are made once or twice per layer and token, so what they check on the way is kept to
+# a few comparisons; a message is put together only for what is refused.
 
 
 def _ints(t, what: str):
     """An int32 device tensor whose last dimension is contiguous."""
-    _need(t.dtype == torch.int32 and (t.numel() == 0 or t.stride(-1) == 1), f"{what}: int32, contiguous rows")
+    if t.dtype != torch.int32 or (t.numel() > 0 and t.stride(-1) != 1):
+        raise ValueError(f"{what}: int32, contiguous rows")
     return t
 
 
-def _rows(t, desc, heads: int, what: str):
+def _rows(t, kind, T: int, heads: int, d: int, what: str):
     """(address, row stride) of a tensor of rows [T, heads*d] or [T, heads, d] with contiguous
     rows, such as a slice of a fused projection's output."""
-    if t.dim() == 3:
-        _need(t.shape[1:] == (heads, desc.d) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == desc.d),
-              f"{what}: [T, {heads}, {desc.d}] with contiguous rows")
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 2:
+        good = shape[0] == T and shape[1] == heads * d and stride[1] == 1
     else:
-        _need(t.dim() == 2 and t.shape[1] == heads * desc.d and t.stride(1) == 1,
-              f"{what}: [T, {heads * desc.d}] with contiguous rows")
-    _need(_DTYPES.get(t.dtype) == desc.dtype, f"{what}: dtype differs from the descriptor's")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else heads * desc.d)
+        good = shape == (T, heads, d) and stride[2] == 1 and (heads == 1 or stride[1] == d)
+    if not good or t.dtype is not kind:
+        raise ValueError(f"{what}: [{T}, {heads * d}] of {kind} with contiguous rows")
+    return t.data_ptr(), (stride[0] if T > 1 else heads * d)
+
+
+def _plain(t, T: int, n: int, what: str):
+    """The address of a contiguous float32 tensor of T*n values, or None."""
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.numel() != T * n or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous float32, {T * n} values")
+    return t.data_ptr()
+
+
+def _status(t):
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.numel() != 1:
+        raise ValueError("status: int32 [1]")
+    return t.data_ptr()
 
 
 def make_rotation(Hq: int, Hkv: int, d: int, dtype: int, inv_freq: torch.Tensor, *,
@@ -347,11 +371,13 @@ def make_rotation(Hq: int, Hkv: int, d: int, dtype: int, inv_freq: torch.Tensor,
     ids, or None for one plane."""
     r = DartRotation()
     sections = [inv_freq.numel()] if sections is None else list(sections)
-    _need(inv_freq.dtype == torch.float32 and inv_freq.is_contiguous(), "inv_freq: contiguous float32")
-    _need(1 <= len(sections) <= 4 and sum(sections) == inv_freq.numel(), "sections: up to 4, summing to the pairs")
+    if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq: contiguous float32")
+    if not 1 <= len(sections) <= 4 or sum(sections) != inv_freq.numel():
+        raise ValueError("sections: up to 4, summing to the pairs")
     for w in (q_weight, k_weight):
-        _need(w is None or (w.numel() == d and w.is_contiguous() and _DTYPES.get(w.dtype) == dtype),
-              "weights: contiguous [d] of the rows' dtype")
+        if w is not None and (w.numel() != d or not w.is_contiguous() or _DTYPES.get(w.dtype) != dtype):
+            raise ValueError("weights: contiguous [d] of the rows' dtype")
     r.Hq, r.Hkv, r.d, r.dtype = Hq, Hkv, d, dtype
     r.rot, r.interleaved, r.planes = 2 * inv_freq.numel(), int(interleaved), len(sections)
     r.sections[:len(sections)] = sections
@@ -359,7 +385,9 @@ def make_rotation(Hq: int, Hkv: int, d: int, dtype: int, inv_freq: torch.Tensor,
     r.q_weight = None if q_weight is None else q_weight.data_ptr()
     r.k_weight = None if k_weight is None else k_weight.data_ptr()
     r.eps, r.scale = eps, scale
+    # the descriptor holds raw device addresses: keep their tensors alive with it
     r._keepalive = (inv_freq, q_weight, k_weight)
+    r._ref, r._heads = C.byref(r), (_KINDS.get(dtype), Hq, Hkv, d, len(sections))
     return r
 
 
@@ -371,11 +399,14 @@ def make_cache(Hq: int, pool: torch.Tensor, pages: torch.Tensor, kv_len: torch.T
     whose memory holds [pages, page_size, Hkv, d] is passed transposed); the value pool is laid out
     like it.  pages: int32 [B, n]; kv_len: int32 [B] with the tokens of the call.  cu_q: int32 [B+1] and T
     tokens, at most max_q of a sequence; without it one token each."""
-    _need(pool.dim() == 4 and pool.stride(3) == 1 and pool.dtype in _DTYPES, "pool: [pages, Hkv, page_size, d]")
-    _need(pages.dim() == 2 and kv_len.numel() == pages.shape[0], "pages: [B, n], kv_len: [B]")
+    if pool.dim() != 4 or pool.stride(3) != 1 or pool.dtype not in _DTYPES:
+        raise ValueError("pool: [pages, Hkv, page_size, d] with contiguous heads")
+    if pages.dim() != 2 or kv_len.numel() != pages.shape[0]:
+        raise ValueError("pages: [B, n], kv_len: [B]")
     c = DartCache()
     c.B, c.Hq, c.Hkv, c.d, c.dtype = pages.shape[0], Hq, pool.shape[1], pool.shape[3], _DTYPES[pool.dtype]
-    _need(cu_q is None or (T is not None and cu_q.numel() == c.B + 1), "cu_q: [B+1], with T")
+    if cu_q is not None and (T is None or cu_q.numel() != c.B + 1):
+        raise ValueError("cu_q: [B+1], with T")
     c.T, c.max_q, c.max_kv = (c.B if T is None else T), max_q, max_kv
     c.cu_q = None if cu_q is None else _ints(cu_q, "cu_q").data_ptr()
     c.kv_len, c.pages = _ints(kv_len, "kv_len").data_ptr(), _ints(pages, "pages").data_ptr()
@@ -386,31 +417,33 @@ def make_cache(Hq: int, pool: torch.Tensor, pages: torch.Tensor, kv_len: torch.T
     c.page_ld = pool.stride(0) if c.n_pages > 1 else 0
     if group_cu is not None:
         c.groups = prefix_len.numel()
-        _need(group_cu.numel() == c.groups + 1 and prefix_pages.dim() == 2 and prefix_pages.shape[0] == c.groups,
-              "group_cu: [groups+1], prefix_pages: [groups, n], prefix_len: [groups]")
+        if group_cu.numel() != c.groups + 1 or prefix_pages.dim() != 2 or prefix_pages.shape[0] != c.groups:
+            raise ValueError("group_cu: [groups+1], prefix_pages: [groups, n], prefix_len: [groups]")
         c.group_cu, c.prefix_len = _ints(group_cu, "group_cu").data_ptr(), _ints(prefix_len, "prefix_len").data_ptr()
         c.prefix_pages = _ints(prefix_pages, "prefix_pages").data_ptr()
         c.prefix_ld = prefix_pages.stride(0) if c.groups > 1 else prefix_pages.shape[1]
         c.max_prefix = max_prefix
     c._keepalive = (pages, kv_len, cu_q, group_cu, prefix_pages, prefix_len)
+    c._ref, c._heads = C.byref(c), (pool.dtype, Hq, c.Hkv, c.d, c.T)
+    c._pool = (pool.shape, pool.stride())
     return c
 
 
-def _pools(cache: DartCache, k_pool, v_pool):
-    for p in (k_pool, v_pool):
-        _need(p.shape == (cache.n_pages, cache.Hkv, cache.page_size, cache.d) and _DTYPES.get(p.dtype) == cache.dtype
-              and (cache.page_size == 1 or p.stride(2) == cache.row_ld)
-              and (cache.Hkv == 1 or p.stride(1) == cache.head_ld)
-              and (cache.n_pages == 1 or p.stride(0) == cache.page_ld) and p.stride(3) == 1,
-              "pools: shape, strides and dtype of the pool the descriptor was made for")
-    return k_pool.data_ptr(), v_pool.data_ptr()
+def _pool(cache: DartCache, p, what: str):
+    shape, stride = cache._pool
+    if p.shape != shape or p.dtype is not cache._heads[0] or (
+            p.stride() != stride and any(a != b for a, b, n in zip(p.stride(), stride, shape) if n > 1)):
+        raise ValueError(f"{what}: shape, strides and dtype of the pool the descriptor was made for")
+    return p.data_ptr()
 
 
 def _planes(pos, planes: int, T: int):
     """(address, plane stride) of position ids [T] or [planes, T], int64."""
-    _need(pos.dtype == torch.int64 and pos.stride(-1) == 1 and pos.numel() == planes * T and pos.shape[-1] == T,
-          "pos: int64 [planes, T]")
-    return pos.data_ptr(), (pos.stride(0) if planes > 1 else 0)
+    shape, stride = pos.shape, pos.stride()
+    if pos.dtype is not torch.int64 or shape[-1] != T or (T > 1 and stride[-1] != 1) or (
+            shape[0] != planes if len(shape) == 2 else planes != 1):
+        raise ValueError(f"pos: int64 [{planes}, {T}]")
+    return pos.data_ptr(), (stride[0] if planes > 1 else 0)
 
 
 def dart_norm_rotate(rotation: DartRotation, q, k, pos, q_out, k_out, *, l1_out=None, stream=None):
@@ -418,31 +451,37 @@ def dart_norm_rotate(rotation: DartRotation, q, k, pos, q_out, k_out, *, l1_out=
     [planes, T]) into q_out and k_out (which may be q and k); l1_out float32 [T]: the L1 norms
     of the key rows."""
     T = q.shape[0]
-    _need(k.shape[0] == T and q_out.shape[0] == T and k_out.shape[0] == T, "rows: T of each")
-    _need(l1_out is None or (l1_out.numel() == T and l1_out.dtype == torch.float32), "l1_out: float32 [T]")
+    kind, Hq, Hkv, d, planes = rotation._heads
+    qp, q_ld = _rows(q, kind, T, Hq, d, "q")
+    kp, k_ld = _rows(k, kind, T, Hkv, d, "k")
+    qo, qo_ld = _rows(q_out, kind, T, Hq, d, "q_out")
+    ko, ko_ld = _rows(k_out, kind, T, Hkv, d, "k_out")
+    pp, p_ld = _planes(pos, planes, T)
+    l1 = _plain(l1_out, T, 1, "l1_out")
     if T == 0:
         return
-    r = rotation
-    _check(lib().dart_norm_rotate(C.byref(r), T, *_rows(q, r, r.Hq, "q"), *_rows(k, r, r.Hkv, "k"),
-                                  *_planes(pos, r.planes, T), *_rows(q_out, r, r.Hq, "q_out"),
-                                  *_rows(k_out, r, r.Hkv, "k_out"), _ptr(l1_out), _stream(stream)),
-           "dart_norm_rotate")
+    _check(lib().dart_norm_rotate(rotation._ref, T, qp, q_ld, kp, k_ld, pp, p_ld, qo, qo_ld, ko, ko_ld, l1,
+                                  _stream(stream)), "dart_norm_rotate")
 
 
 def dart_norm_rotate_append(rotation: DartRotation, cache: DartCache, q, k, v, pos, q_out, k_pool, v_pool, *,
                             k_out=None, l1_out=None, status=None, stream=None):
     """dart_norm_rotate for the tokens of `cache`, keys and values going to their pages.  status:
     int32 [1] that bits are OR-ed into, or None."""
-    T, r = cache.T, rotation
-    _need(all(x is None or x.shape[0] == T for x in (q, k, v, q_out, k_out)), "rows: T of each")
-    _need(l1_out is None or (l1_out.numel() == T and l1_out.dtype == torch.float32), "l1_out: float32 [T]")
+    kind, Hq, Hkv, d, planes = rotation._heads
+    T = cache._heads[4]
+    qp, q_ld = _rows(q, kind, T, Hq, d, "q")
+    kp, k_ld = _rows(k, kind, T, Hkv, d, "k")
+    vp, v_ld = _rows(v, kind, T, Hkv, d, "v")
+    qo, qo_ld = _rows(q_out, kind, T, Hq, d, "q_out")
+    ko, ko_ld = (None, 0) if k_out is None else _rows(k_out, kind, T, Hkv, d, "k_out")
+    pp, p_ld = _planes(pos, planes, T)
+    k_at, v_at = _pool(cache, k_pool, "k_pool"), _pool(cache, v_pool, "v_pool")
+    l1, st = _plain(l1_out, T, 1, "l1_out"), _status(status)
     if T == 0:
         return
-    ko = (None, 0) if k_out is None else _rows(k_out, r, r.Hkv, "k_out")
-    _check(lib().dart_norm_rotate_append(
-        C.byref(r), C.byref(cache), *_rows(q, r, r.Hq, "q"), *_rows(k, r, r.Hkv, "k"), *_rows(v, r, r.Hkv, "v"),
-        *_planes(pos, r.planes, T), *_rows(q_out, r, r.Hq, "q_out"), *ko, _ptr(l1_out),
-        *_pools(cache, k_pool, v_pool), _ptr(status), _stream(stream)), "dart_norm_rotate_append")
+    _check(lib().dart_norm_rotate_append(rotation._ref, cache._ref, qp, q_ld, kp, k_ld, vp, v_ld, pp, p_ld, qo, qo_ld,
+                                         ko, ko_ld, l1, k_at, v_at, st, _stream(stream)), "dart_norm_rotate_append")
 
 
 def dart_attend_workspace_bytes(cache: DartCache) -> int:
@@ -460,12 +499,12 @@ def dart_attend(cache: DartCache, q, k_pool, v_pool, out, ws, *, scale: float, c
                 status=None, stream=None):
     """Attention of the tokens' queries q [T, Hq*d] over the cache (and the shared prefixes) into
     out [T, Hq*d]; lse float32 [T, Hq]."""
-    T, c = cache.T, cache
-    _need(q.shape[0] == T and out.shape[0] == T, "rows: T of each")
-    _need(lse is None or (lse.numel() == T * c.Hq and lse.dtype == torch.float32 and lse.is_contiguous()),
-          "lse: float32 [T, Hq]")
+    kind, Hq, _, d, T = cache._heads
+    qp, q_ld = _rows(q, kind, T, Hq, d, "q")
+    o, o_ld = _rows(out, kind, T, Hq, d, "out")
+    k_at, v_at = _pool(cache, k_pool, "k_pool"), _pool(cache, v_pool, "v_pool")
+    le, st = _plain(lse, T, Hq, "lse"), _status(status)
     if T == 0:
         return
-    _check(lib().dart_attend(C.byref(c), *_rows(q, c, c.Hq, "q"), *_pools(c, k_pool, v_pool), scale, int(causal),
-                             *_rows(out, c, c.Hq, "out"), _ptr(lse), _ptr(ws), ws.numel(), _ptr(status),
+    _check(lib().dart_attend(cache._ref, qp, q_ld, k_at, v_at, scale, causal, o, o_ld, le, ws.data_ptr(), ws.numel(), st,
                              _stream(stream)), "dart_attend")

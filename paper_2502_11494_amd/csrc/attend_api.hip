@@ -19,7 +19,7 @@ constexpr int64_t kMaxLd = int64_t(1) << 24;       // row strides of q, k, v and
 constexpr int64_t kMaxPoolLd = int64_t(1) << 40;   // strides inside the pools, elements
 constexpr int kMaxSequences = 1 << 20, kMaxTokens = 1 << 24, kMaxKeys = 1 << 27, kMaxPage = 1 << 20;
 constexpr int kMaxHeads = 1024, kMaxHead = 256;
-constexpr long kMaxSlots = (1 << 23) - 1;          // row tiles of one launch
+constexpr long kMaxRows = 1L << 28, kMaxBlocks = (1L << 23) - 1;  // (token, head) pairs of a key head; blocks of a launch
 
 inline bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 inline int elem(int dtype) { return dtype == DART_BF16 ? 2 : 4; }
@@ -167,51 +167,58 @@ dart_status set_rows(Rotate& a, int dtype, int T, const void* q, int64_t q_ld, c
 }
 
 // ---- attention: which tiles, how many parts ---------------------------------------------------
-enum Kind { kFew, kMany, kWide };  // 32 rows, the keys dealt to four waves; 128 rows; 256 rows
-
-struct Launch {
-  Kind kind;
-  int bm, chunk, chunks;
-  long slots;
-};
+enum Kind { kFew, kMany, kWide };  // 16 rows, the keys dealt to four waves; 128 rows; 256 rows
 
 struct AttendPlan {
-  Launch own, pre;
+  Kind own_kind, pre_kind;
+  Parting own, pre;
   int parts;
-  size_t o_o, o_ml, total;
+  size_t o_ml, total;
 };
 
-int rows_of(Kind k) { return k == kFew ? 32 : k == kMany ? 128 : 256; }
+int rows_of(Kind k) { return k == kFew ? 16 : k == kMany ? 128 : 256; }
+long blocks_of(const Cache& c, const Parting& p) { return p.slots * c.Hkv * p.chunks; }
 
 // rows: (token, head) pairs of a sequence or group at most; owners: how many of them.
-Launch plan_launch(const Cache& c, int dtype, long rows, int owners, int max_keys) {
-  Launch l;
+Kind plan_parting(const Cache& c, int dtype, bool prefix, long rows, int owners, int max_keys, Parting& p) {
   const int r = c.Hq / c.Hkv;
-  l.kind = rows <= 32 ? kFew : rows <= 128 || dtype == DART_F32 || c.d > 128 ? kMany : kWide;
-  if (dtype == DART_F32 && c.d > 128) l.kind = kMany;
-  l.bm = rows_of(l.kind);
-  l.slots = (long)c.T * r / l.bm + owners;
-  const long blocks = std::max(1L, std::min(l.slots, (long)owners * ((rows + l.bm - 1) / l.bm)) * c.Hkv);
+  // 256-row tiles take the least from LDS and caches per row, where there are enough of them for the chip
+  const bool wide = dtype == DART_BF16 && c.d <= 128 && ((long)c.T * r / 256) * c.Hkv >= 512;
+  Kind kind = rows <= 32 ? kFew : wide && rows > 128 ? kWide : kMany;
+  if (dtype == DART_F32 && c.d > 128) kind = kMany;
+  const int bm = rows_of(kind);
+  p = {};
+  p.prefix = prefix;
+  p.few = kind == kFew;
+  if (!prefix && !c.cu) {
+    p.per_owner = (r + bm - 1) / bm;
+    p.slots = (long)owners * p.per_owner;
+  } else {
+    p.slots = (long)c.T * r / bm + owners;
+  }
+  const long blocks = std::max(1L, std::min(p.slots, (long)owners * ((rows + bm - 1) / bm)) * c.Hkv);
   // enough parts to fill the chip twice, of 256 keys at least
   const long want = std::max(1L, 512 / blocks);
-  long chunk = (max_keys + want - 1) / want;
-  chunk = std::max(256L, (chunk + 255) / 256 * 256);
-  l.chunk = (int)chunk;
-  l.chunks = std::max(1, (int)((max_keys + chunk - 1) / chunk));
-  return l;
+  const long chunk = std::max(256L, ((max_keys + want - 1) / want + 255) / 256 * 256);
+  p.chunk = (int)chunk;
+  p.chunks = std::max(1, (int)((max_keys + chunk - 1) / chunk));
+  return kind;
 }
 
 dart_status plan_attend(const Cache& c, int dtype, AttendPlan& p) {
   const int r = c.Hq / c.Hkv;
+  if ((long)c.T * r > kMaxRows) return DART_ERR_SHAPE;
   p = {};
-  p.own = plan_launch(c, dtype, (long)c.max_q * r, c.B, c.max_kv);
+  p.own_kind = plan_parting(c, dtype, false, (long)c.max_q * r, c.B, c.max_kv, p.own);
   p.parts = p.own.chunks;
   if (c.groups > 0) {
     const long rows = std::min((long)c.T, (long)c.max_q * c.B) * r;
-    p.pre = plan_launch(c, dtype, std::max(1L, (rows + c.groups - 1) / c.groups), c.groups, c.max_prefix);
+    p.pre_kind = plan_parting(c, dtype, true, std::max(1L, (rows + c.groups - 1) / c.groups), c.groups, c.max_prefix, p.pre);
     p.parts += p.pre.chunks;
+    p.own.first_part = p.pre.chunks;
   }
-  if (p.own.slots > kMaxSlots || p.pre.slots > kMaxSlots || p.parts > 65535) return DART_ERR_SHAPE;
+  if (blocks_of(c, p.own) > kMaxBlocks || blocks_of(c, p.pre) > kMaxBlocks) return DART_ERR_SHAPE;
+  p.own.parts = p.pre.parts = p.parts;
   auto up = [](size_t v) { return (v + kAlign - 1) / kAlign * kAlign; };
   const size_t rows = (size_t)c.T * c.Hq;
   p.total = kAlign;
@@ -222,32 +229,32 @@ dart_status plan_attend(const Cache& c, int dtype, AttendPlan& p) {
   return DART_OK;
 }
 
-template <int DT, int DP, int WM, int WK, int QT, int KT>
-dart_status launch_tiles(const Attend& a, const Cache& c, const Parting& sp, const Launch& l, hipStream_t st) {
-  typedef AttendShape<DT, DP, WM, WK, QT, KT> S;
-  k_attend<DT, DP, WM, WK, QT, KT><<<dim3((unsigned)l.slots, c.Hkv, l.chunks), dim3(S::kThreads), S::kLds, st>>>(a, c, sp);
+template <int DT, int DP, int QW, int WM, int WK, int KT>
+dart_status launch_tiles(const Attend& a, const Cache& c, const Parting& sp, hipStream_t st) {
+  typedef AttendShape<DT, DP, QW, WM, WK, KT> S;
+  k_attend<DT, DP, QW, WM, WK, KT><<<dim3((unsigned)blocks_of(c, sp)), dim3(S::kThreads), S::kLds, st>>>(a, c, sp);
   return launched();
 }
 
 template <int DP>
-dart_status launch_bf16(const Attend& a, const Cache& c, const Parting& sp, const Launch& l, hipStream_t st) {
-  if (l.kind == kFew) return launch_tiles<kBF16, DP, 1, 4, 1, 32>(a, c, sp, l, st);
+dart_status launch_bf16(const Attend& a, const Cache& c, const Parting& sp, Kind kind, hipStream_t st) {
+  if (kind == kFew) return launch_tiles<kBF16, DP, 16, 1, 4, 32>(a, c, sp, st);
   if constexpr (DP <= 128)
-    if (l.kind == kWide) return launch_tiles<kBF16, DP, 4, 1, 2, 64>(a, c, sp, l, st);
-  return launch_tiles<kBF16, DP, 4, 1, 1, 64>(a, c, sp, l, st);
+    if (kind == kWide) return launch_tiles<kBF16, DP, 32, 8, 1, 64>(a, c, sp, st);
+  return launch_tiles<kBF16, DP, 32, 4, 1, 64>(a, c, sp, st);
 }
 
 template <int DP>
-dart_status launch_f32(const Attend& a, const Cache& c, const Parting& sp, const Launch& l, hipStream_t st) {
+dart_status launch_f32(const Attend& a, const Cache& c, const Parting& sp, Kind kind, hipStream_t st) {
   if constexpr (DP <= 128)
-    if (l.kind == kFew) return launch_tiles<kF32, DP, 1, 4, 1, 32>(a, c, sp, l, st);
-  return launch_tiles<kF32, DP, 4, 1, 1, 32>(a, c, sp, l, st);
+    if (kind == kFew) return launch_tiles<kF32, DP, 16, 1, 4, 32>(a, c, sp, st);
+  return launch_tiles<kF32, DP, 32, 4, 1, 32>(a, c, sp, st);
 }
 
-dart_status launch_attend(const Attend& a, const Cache& c, int dtype, const Parting& sp, const Launch& l, hipStream_t st) {
+dart_status launch_attend(const Attend& a, const Cache& c, int dtype, const Parting& sp, Kind k, hipStream_t st) {
   if (dtype == DART_BF16)
-    return c.d <= 64 ? launch_bf16<64>(a, c, sp, l, st) : c.d <= 128 ? launch_bf16<128>(a, c, sp, l, st) : launch_bf16<256>(a, c, sp, l, st);
-  return c.d <= 64 ? launch_f32<64>(a, c, sp, l, st) : c.d <= 128 ? launch_f32<128>(a, c, sp, l, st) : launch_f32<256>(a, c, sp, l, st);
+    return c.d <= 64 ? launch_bf16<64>(a, c, sp, k, st) : c.d <= 128 ? launch_bf16<128>(a, c, sp, k, st) : launch_bf16<256>(a, c, sp, k, st);
+  return c.d <= 64 ? launch_f32<64>(a, c, sp, k, st) : c.d <= 128 ? launch_f32<128>(a, c, sp, k, st) : launch_f32<256>(a, c, sp, k, st);
 }
 
 }  // namespace
@@ -315,11 +322,13 @@ dart_status dart_attend(const dart_cache* cache, const void* q, int64_t q_ld, co
   if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < p.total) return DART_ERR_WORKSPACE;
   c.status = status;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const Attend a = {q, k_pool, v_pool, out, lse, q_ld, out_ld, scale, causal != 0};
+  const Attend a = {q, k_pool, v_pool, out, lse, q_ld, out_ld, scale, causal != 0, 1.0 / (c.Hq / c.Hkv)};
   float* part_o = static_cast<float*>(ws);
   float2* part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(ws) + p.o_ml);
-  if (c.groups > 0) DART_TRY(launch_attend(a, c, cache->dtype, {1, p.pre.chunk, 0, p.parts, part_o, part_ml}, p.pre, st));
-  DART_TRY(launch_attend(a, c, cache->dtype, {0, p.own.chunk, p.pre.chunks, p.parts, part_o, part_ml}, p.own, st));
+  p.own.part_o = p.pre.part_o = part_o;
+  p.own.part_ml = p.pre.part_ml = part_ml;
+  if (c.groups > 0) DART_TRY(launch_attend(a, c, cache->dtype, p.pre, p.pre_kind, st));
+  DART_TRY(launch_attend(a, c, cache->dtype, p.own, p.own_kind, st));
   if (p.parts == 1) return DART_OK;
   int lanes_shift = 0;
   while ((4 << lanes_shift) < c.d) ++lanes_shift;

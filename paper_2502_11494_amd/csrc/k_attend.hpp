@@ -22,56 +22,71 @@ struct Attend {
   long q_ld, out_ld;
   float scale;
   int causal;
+  double per_token;  // 1 / (rows of a token: query heads of a key head)
 };
 
-// How a launch divides its keys, and where its results go.  A row's results are joined from `parts`
-// partial ones (running sum, maximum and weighted values of some of its keys each), or written at
-// once where there is one.
+// row / rows of a token, exactly: rows are below 2^28.
+__device__ __forceinline__ int token_in(const Attend& a, int row) { return (int)(((double)row + 0.5) * a.per_token); }
+
+// How the keys of a launch are divided, and where its results go.  A row's results are joined from
+// `parts` partial ones (running sum, maximum and weighted values of some of its keys each), or written
+// at once where there is one.
 struct Parting {
   int prefix;      // the keys are the groups' shared prefixes (else each sequence's own)
+  int few;         // tiles of 32 rows, the keys dealt to four waves (else four waves of rows)
   int chunk;       // keys of a part
-  int first_part;  // part number of the launch's first chunk
+  int chunks;
+  int first_part;  // part number of the first chunk
   int parts;
+  int per_owner;   // tiles of a sequence where each has one token; 0: see slot_owner
+  long slots;      // row tiles
   float* part_o;   // [parts][T*Hq][d]
   float2* part_ml; // [parts][T*Hq]: maximum (of scores times log2 e), sum
 };
 
 // ---- the arithmetic of a wave ----------------------------------------------------------------
-// 32 queries lie in the columns of a 32x32 tile (lane % 32), 32 keys in its rows: a lane holds of
-// its query the 16 keys 8*(i/4) + 4*(lane/32) + i%4.  So the maximum and the sum of a query are within
-// a lane but for one exchange with lane ^ 32; the weights are, rounded, the right operand of the
-// second product as they stand (its sum over keys does not mind their order, as long as the
-// values are read in the same one), and its result has the queries in the columns again, so that
-// rescaling it is a product by a number of the lane's own.
-template <int DT>
-struct Math;
-
+// QW queries (32, or 16 where a block has no more) lie in the columns of a matrix tile, lane % QW, and its
+// keys in the rows, so that each of the kGroups groups of QW lanes holds, of every query, one run of four
+// keys in 4 * kGroups.  The maximum and the sum of a query are then within a lane but for an exchange
+// between the groups; the weights are, rounded, the right operand of the second product as they
+// stand (its sum over keys does not mind their order, as long as the values are read in the same one),
+// and its result has the queries in the columns again, so that rescaling it is a product by a number
+// of the lane's own.
+template <int QW>
+struct Acc { typedef f32x16 type; };
 template <>
-struct Math<kBF16> {
-  static constexpr int kVec = 8;                       // elements of a 16-byte piece
-  typedef bf16x8 QFrag;
-  template <int DP>
-  static constexpr int steps() { return DP / 16; }     // of the first product
-  // 8 elements from 16*s + 8*half of query or key `row`
-  __device__ static __forceinline__ int piece(int s, int half) { return 2 * s + half; }
-  __device__ static __forceinline__ f32x16 qk(const QFrag& k, const QFrag& q, f32x16 acc) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q, acc, 0, 0, 0);
-  }
-};
+struct Acc<16> { typedef f32x4v type; };
 
-template <>
-struct Math<kF32> {
-  static constexpr int kVec = 4;
-  typedef f32x4v QFrag;
+template <int DT, int QW>
+struct Math {
+  typedef typename Acc<QW>::type acc;
+  static constexpr int kVec = DT == kBF16 ? 8 : 4;           // elements of a 16-byte piece
+  static constexpr int kGroups = 64 / QW, kRegs = QW * QW / 64;
+  static constexpr int kScores = QW / 2;                     // of a lane, for 32 keys
+  static constexpr int kTiles = 32 / QW;                     // of 32 keys
+  static constexpr int kRun = 4 * kGroups;
+  // what score (or row of a result tile) number u of a lane of group g is of
+  __device__ static __forceinline__ constexpr int place(int u, int g) { return kRun * (u / 4) + 4 * g + u % 4; }
+  // key and query pieces of step s: number kGroups * s + g of the row
   template <int DP>
-  static constexpr int steps() { return DP / 8; }
-  __device__ static __forceinline__ int piece(int s, int half) { return 2 * s + half; }
-  // (four products of two elements each: element j of both halves' pieces)
-  __device__ static __forceinline__ f32x16 qk(const QFrag& k, const QFrag& q, f32x16 acc) {
+  static constexpr int steps() { return DP / (kVec * kGroups); }
+  __device__ static __forceinline__ acc qk(const u32x4& k, const u32x4& q, acc c) {
+    if constexpr (DT == kBF16) {
+      const bf16x8 x = __builtin_bit_cast(bf16x8, k), y = __builtin_bit_cast(bf16x8, q);
+      if constexpr (QW == 32) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
+      else c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(k[j], q[j], acc, 0, 0, 0);
-    return acc;
+      for (int j = 0; j < 4; ++j) c = av(__uint_as_float(k[j]), __uint_as_float(q[j]), c);
+    }
+    return c;
   }
+  // (32-bit rows) one key of each group by one weight of each group
+  __device__ static __forceinline__ acc av(float v, float p, acc c) {
+    if constexpr (QW == 32) return __builtin_amdgcn_mfma_f32_32x32x2f32(v, p, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x4f32(v, p, c, 0, 0, 0);
+  }
+  __device__ static __forceinline__ acc pv(const u32x4& v, const u32x4& p, acc c) { return qk(v, p, c); }
 };
 
 // Rows of a tile in LDS lie at multiples of their length, their 16-byte pieces permuted by the row
@@ -82,33 +97,40 @@ __device__ __forceinline__ int mix(int row) {
   return RB == 128 ? (((row >> 1) & 1) << 2) | ((row >> 2) & 3) : ((row & 3) << 2) | ((row >> 2) & 3);
 }
 
-__device__ __forceinline__ float other_half_max(float x) {
+// Over the lanes that hold the same query.
+template <int QW>
+__device__ __forceinline__ float groups_max(float x) {
+  if constexpr (QW == 16) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
   auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ float other_half_sum(float x) {
+template <int QW>
+__device__ __forceinline__ float groups_sum(float x) {
+  if constexpr (QW == 16) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
   auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Puts 0 in the place of infinities and NaN; not 0 if there were any.  (An exponent of ones carries into
+// the bit above it.)
 template <int DT>
-__device__ __forceinline__ bool finite_piece(const u32x4& v) {
-  bool bad = false;
+__device__ __forceinline__ uint32_t drop_infinities(u32x4& v) {
+  uint32_t any = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (DT == kBF16) bad |= (v[i] & 0x7f80u) == 0x7f80u || (v[i] & 0x7f800000u) == 0x7f800000u;
-    else bad |= (v[i] & 0x7f800000u) == 0x7f800000u;
+    const uint32_t hi = ((v[i] & 0x7f800000u) + 0x00800000u) >> 31;
+    const uint32_t lo = DT == kBF16 ? ((v[i] & 0x7f80u) + 0x80u) >> 15 : 0u;
+    any |= hi | lo;
+    v[i] &= DT == kBF16 ? ~((0u - hi) << 16 | ((0u - lo) >> 16)) : ~(0u - hi);
   }
-  return !bad;
+  return any;
 }
-// The rows of one block, and the keys they are taken against.
-struct Tile {
-  int tok0;          // first token of the sequence (or group)
-  int rows;          // (token, head of the key head's group) pairs of it: token-major
-  int n, kv;         // tokens; keys
-  int shift;         // causal: token i sees keys up to kv - n + i; else unused
-  const int* table;  // pages
-};
 
 __device__ __forceinline__ int token_of(const Cache& c, int b) {
   if (c.cu == nullptr) return b < c.B ? b : c.B;
@@ -116,11 +138,12 @@ __device__ __forceinline__ int token_of(const Cache& c, int b) {
   return t < 0 ? 0 : t < c.T ? t : c.T;
 }
 
-// Tile slot -> (sequence or group, tile).  Sequence i of `count` owns the slots from start(i) =
-// floor(first token * r / bm) + i on: at least as many as it has tiles, whatever its length, and found
-// without a sum over the sequences before it.
+// Tile slot -> sequence (or group).  Sequence i of `count` owns the slots from floor(first token * r /
+// BM) + i on: at least as many as it has tiles, whatever its length, and found without a sum over the
+// sequences before it.
 template <int BM>
 __device__ __forceinline__ int slot_owner(const Cache& c, const int* group_cu, int count, int r, long slot) {
+  if (count == 1) return 0;
   const int lane = threadIdx.x & 63;
   int from = 0, left = count;
   while (true) {
@@ -136,8 +159,8 @@ __device__ __forceinline__ int slot_owner(const Cache& c, const int* group_cu, i
   }
 }
 
-// WM waves along the rows (QT tiles of 32 each) by WK along the keys; a step takes KT keys per key group.
-template <int DT, int DP, int WM, int WK, int QT, int KT>
+// WM waves along the rows, QW each, by WK along the keys; a step takes KT keys per key group.
+template <int DT, int DP, int QW, int WM, int WK, int KT>
 struct AttendShape {
   static constexpr int kEsz = DT == kBF16 ? 2 : 4;
   static constexpr int kRowBytes = DP * kEsz;
@@ -148,376 +171,342 @@ struct AttendShape {
   static constexpr int kApart = kGroup / kPieces;        // rows between a thread's pieces
   static constexpr int kBuffers = WM > 1 ? 2 : 1;
   static constexpr int kTileBytes = KT * kRowBytes;
-  static constexpr int kBM = 32 * WM * QT;
+  static constexpr int kBM = QW * WM;
   static constexpr int kLds = WK * kBuffers * 2 * kTileBytes;
   static_assert(kGroup % kPieces == 0 && KT * kPieces % kGroup == 0 && KT % 32 == 0, "");
-  static_assert(WK == 1 || (QT == 1 && WM == 1), "");
-  static_assert(WK == 1 || 32 * DP * 4 <= kBuffers * 2 * kTileBytes, "joined in the tiles' place");
+  static_assert(WK == 1 || WM == 1, "");
+  static_assert(WK == 1 || QW * DP * 4 <= kBuffers * 2 * kTileBytes, "joined in the tiles' place");
 };
 
-template <int DT, int DP, int WM, int WK, int QT, int KT>
-__global__ __launch_bounds__(64 * WM * WK) void k_attend(Attend a, Cache c, Parting sp) {
-  typedef AttendShape<DT, DP, WM, WK, QT, KT> S;
-  typedef Math<DT> M;
-  typedef typename M::QFrag QFrag;
-  constexpr int kSteps = M::template steps<DP>(), kDT = DP / 32, kSub = KT / 32, RB = S::kRowBytes;
-  extern __shared__ __align__(16) unsigned char lds[];
-  __shared__ int odd_values[4];
-  __shared__ float2 joined[WK + 1][32];
+// What a block keeps in LDS beside the tiles.
+struct AttendShared {
+  int odd_values[4];
+  float2 joined[5][32];
+};
 
+// One block: row tile `slot` against chunk `part` of the keys of head `head`.
+template <int DT, int DP, int QW, int WM, int WK, int KT>
+__device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, const Parting& sp, unsigned char* lds, AttendShared& sh,
+                                            long slot, int head, int part) {
+  typedef AttendShape<DT, DP, QW, WM, WK, KT> S;
+  typedef Math<DT, QW> M;
+  typedef typename M::acc acc;
+  constexpr int kSteps = M::template steps<DP>(), kDT = DP / QW, kSub = KT / 32, RB = S::kRowBytes;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave % WM, wk = wave / WM;
-  const int half = lane >> 5, col = lane & 31;
-  const int r = c.Hq / c.Hkv, head = blockIdx.y;
+  const int grp = lane / QW, col = lane % QW;
+  const int r = c.Hq / c.Hkv;
 
-  // ---- whose rows, which keys
-  Tile tl;
-  int tile;
-  {
-    const long slot = (long)gridDim.x - 1 - blockIdx.x;  // the tiles that see most keys first
-    if (sp.prefix) {
-      const int g = slot_owner<S::kBM>(c, c.group_cu, c.groups, r, slot);
-      const int b0 = c.group_cu[g], b1 = c.group_cu[g + 1];
-      const int n = prefix_of(c, g);
-      const bool ok = n >= 0;
-      if (!ok && threadIdx.x == 0) flag(c, kBadSequence);
-      tl.tok0 = token_of(c, b0 < 0 ? 0 : b0 < c.B ? b0 : c.B);
-      tl.n = ok ? token_of(c, b1) - tl.tok0 : 0;
-      tl.kv = ok ? n : 0;
-      tl.table = c.prefix_pages + (long)g * c.prefix_ld;
-      tile = (int)(slot - ((long)tl.tok0 * r / S::kBM + g));
-    } else {
-      const int b = slot_owner<S::kBM>(c, nullptr, c.B, r, slot);
-      const Seq s = sequence_of(c, b);
-      if (!s.valid && threadIdx.x == 0) flag(c, kBadSequence);
-      tl.tok0 = s.tok0;
-      tl.n = s.n;
-      tl.kv = s.kv;
-      tl.table = c.pages + (long)b * c.pages_ld;
-      tile = (int)(slot - ((long)s.tok0 * r / S::kBM + b));
-    }
-    tl.rows = tl.n > 0 ? tl.n * r : 0;
+  // ---- whose rows (token-major pairs of a token and a head of the key head's group), which keys
+  int tok0, n, kv, tile;
+  const int* table;
+  if (sp.prefix) {
+    const int g = slot_owner<S::kBM>(c, c.group_cu, c.groups, r, slot);
+    const int b0 = c.group_cu[g], b1 = c.group_cu[g + 1];
+    const int keys = prefix_of(c, g);
+    if (keys < 0 && threadIdx.x == 0) flag(c, kBadSequence);
+    tok0 = token_of(c, b0 < 0 ? 0 : b0 < c.B ? b0 : c.B);
+    n = keys >= 0 ? token_of(c, b1) - tok0 : 0;
+    kv = keys >= 0 ? keys : 0;
+    table = c.prefix_pages + (long)g * c.prefix_ld;
+    tile = (int)(slot - ((long)tok0 * r / S::kBM + g));
+  } else {
+    const int b = sp.per_owner ? (int)slot / sp.per_owner : slot_owner<S::kBM>(c, nullptr, c.B, r, slot);
+    const Seq s = sequence_of(c, b);
+    if (!s.valid && threadIdx.x == 0) flag(c, kBadSequence);
+    tok0 = s.tok0;
+    n = s.n;
+    kv = s.kv;
+    table = c.pages + (long)b * c.pages_ld;
+    tile = sp.per_owner ? (int)slot % sp.per_owner : (int)(slot - ((long)tok0 * r / S::kBM + b));
   }
-  const int row0 = tile * S::kBM;
-  if (tile < 0 || row0 >= tl.rows) return;
+  const int rows = n > 0 ? n * r : 0, row0 = tile * S::kBM;
+  if (tile < 0 || row0 >= rows) return;
   const bool causal = a.causal && !sp.prefix;
-  const int last_tok = ((row0 + S::kBM < tl.rows ? row0 + S::kBM : tl.rows) - 1) / r;
-  int k1 = causal && tl.kv - tl.n + last_tok + 1 < tl.kv ? tl.kv - tl.n + last_tok + 1 : tl.kv;
-  const int k0 = blockIdx.z * sp.chunk;
-  if (k1 - k0 > sp.chunk) k1 = k0 + sp.chunk;
-  if (k1 <= k0 && (sp.parts > 1 || blockIdx.z > 0)) return;
+  int k1 = kv;
+  if (causal) k1 = min(kv, kv - n + token_in(a, min(row0 + S::kBM, rows) - 1) + 1);
+  const int k0 = part * sp.chunk;
+  k1 = min(k1, k0 + sp.chunk);
+  if (k1 <= k0 && (sp.parts > 1 || part > 0)) return;
 
-  // ---- this wave's queries: the last key each of them sees, and their pieces
-  QFrag q[QT][kSteps];
-  int lim[QT], tok[QT], qh[QT];
-  const uint32_t flip = a.scale < 0.f ? (DT == kBF16 ? 0x80008000u : 0x80000000u) : 0u;  // (scores then scale by |scale|)
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int row = row0 + (wm * QT + t) * 32 + col;
-    const bool in = row < tl.rows;
-    const int i = (in ? row : tl.rows - 1) / r;
-    tok[t] = in ? tl.tok0 + i : -1;
-    qh[t] = head * r + (in ? row : tl.rows - 1) - i * r;
-    lim[t] = causal ? tl.kv - tl.n + i : tl.kv - 1;
-    if (lim[t] > k1 - 1) lim[t] = k1 - 1;
-    const long at = (long)(tl.tok0 + i) * a.q_ld + (long)qh[t] * c.d;
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const int e = M::piece(s, half) * M::kVec;
-      u32x4 v = {0, 0, 0, 0};
-      if (e < c.d && a.scale != 0.f) {
-        v = *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(a.q) + (at + e) * S::kEsz);
-        v ^= flip;
-      }
-      q[t][s] = __builtin_bit_cast(QFrag, v);
-    }
-  }
-  // (scale 0: queries of zeros, so that a hidden score stays -infinity)
-  const float scale2 = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;
-  const int lim_first = __builtin_amdgcn_readfirstlane(lim[0]);                 // of the wave's rows
-  const int lim_block = causal ? min(tl.kv - tl.n + row0 / r, k1 - 1) : k1 - 1;  // of the block's
-
-  // ---- staging: pieces of keys and values, through registers into LDS
+  // ---- staging: pieces of keys and values, through registers into LDS.  Loads are unconditional: what lies
+  // past the keys (or the head) is read again from the last of them, and put right as it goes to LDS.
   const int gt = threadIdx.x - wk * S::kGroup;
   const int my_row = gt / S::kPieces, my_piece = gt % S::kPieces;
   const bool my_on = my_piece * M::kVec < c.d;
-  const unsigned char* kp = static_cast<const unsigned char*>(a.k_pool) + ((long)head * c.head_ld + my_piece * M::kVec) * S::kEsz;
-  const unsigned char* vp = static_cast<const unsigned char*>(a.v_pool) + ((long)head * c.head_ld + my_piece * M::kVec) * S::kEsz;
+  const long piece_at = ((long)head * c.head_ld + (my_on ? my_piece * M::kVec : 0)) * S::kEsz;
+  const unsigned char* kp = static_cast<const unsigned char*>(a.k_pool) + piece_at;
+  const unsigned char* vp = static_cast<const unsigned char*>(a.v_pool) + piece_at;
   unsigned char* const my_lds = lds + wk * (S::kBuffers * 2 * S::kTileBytes);
-  const int row_mask = (1 << c.page_shift) - 1;
+  const int row_mask = (1 << c.page_shift) - 1, last_key = k1 - 1;
   u32x4 kr[S::kLoads], vr[S::kLoads];
   int pg[S::kLoads];
   bool bad_page = false;
   auto load_pages = [&](int kb) {
 #pragma unroll
-    for (int i = 0; i < S::kLoads; ++i) {
-      const int key = kb + my_row + i * S::kApart;
-      pg[i] = key < k1 ? tl.table[key >> c.page_shift] : 0;
-    }
+    for (int i = 0; i < S::kLoads; ++i) pg[i] = table[min(kb + my_row + i * S::kApart, last_key) >> c.page_shift];
   };
   auto load_tile = [&](int kb) {
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
-      const int key = kb + my_row + i * S::kApart;
-      kr[i] = u32x4{0, 0, 0, 0};
-      vr[i] = u32x4{0, 0, 0, 0};  // (what lies behind the keys may be anything; its weight is 0, and 0 times NaN is NaN)
       int page = pg[i];
       if ((unsigned)page >= (unsigned)c.n_pages) page = 0, bad_page = true;
-      const long off = ((long)page * c.page_ld + (long)(key & row_mask) * c.row_ld) * S::kEsz;
-      if (key < k1 && my_on) {
-        kr[i] = *reinterpret_cast<const u32x4*>(kp + off);
-        vr[i] = *reinterpret_cast<const u32x4*>(vp + off);
-      }
+      const int row = min(kb + my_row + i * S::kApart, last_key) & row_mask;
+      const long off = ((long)page * c.page_ld + (long)row * c.row_ld) * S::kEsz;
+      kr[i] = *reinterpret_cast<const u32x4*>(kp + off);
+      vr[i] = *reinterpret_cast<const u32x4*>(vp + off);
     }
   };
-  auto store_tile = [&](unsigned char* buf, int kb, int it) {
-    if (causal && kb + KT - 1 > lim_block) {
-      // Some row does not see some of these keys.  Their weight is 0 there, but its product with a value
-      // that is no number would be none either: such a tile is taken key by key (below).
-      bool fine = true;
+  const int steps = (k1 - k0 + KT * WK - 1) / (KT * WK);
+  const int kstep = KT * WK, kfirst = k0 + wk * KT;
+  if (steps > 0) load_pages(kfirst);
+
+  // ---- this lane's query: the last key it sees, and its pieces
+  const int my = row0 + wm * QW + col;
+  const bool in = my < rows;
+  const int mine = in ? my : rows - 1, my_tok = token_in(a, mine);
+  const int qh = head * r + mine - my_tok * r;
+  const int lim = causal ? min(kv - n + my_tok, last_key) : last_key;
+  const uint32_t flip = a.scale < 0.f ? (DT == kBF16 ? 0x80008000u : 0x80000000u) : 0u;  // (scores then scale by |scale|)
+  const unsigned char* q_at =
+      static_cast<const unsigned char*>(a.q) + ((long)(tok0 + my_tok) * a.q_ld + (long)qh * c.d) * S::kEsz;
+  u32x4 q[kSteps];
 #pragma unroll
-      for (int i = 0; i < S::kLoads; ++i) fine = fine && finite_piece<DT>(vr[i]);
-      if (!fine) odd_values[(WM > 1 ? it : wk) & 3] = 1;
+  for (int s = 0; s < kSteps; ++s) {
+    const int e = (M::kGroups * s + grp) * M::kVec;
+    u32x4 v = *reinterpret_cast<const u32x4*>(q_at + (e < c.d ? e : 0) * S::kEsz);
+    // (scale 0: queries of zeros, so that a hidden score stays -infinity)
+    v = e < c.d && a.scale != 0.f ? v ^ flip : u32x4{0, 0, 0, 0};
+    q[s] = v;
+  }
+  const float scale2 = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;
+  const int lim_first = __builtin_amdgcn_readfirstlane(lim);                              // of the wave's rows
+  const int lim_block = causal ? min(kv - n + token_in(a, row0), last_key) : last_key;    // of the block's
+
+  auto store_tile = [&](unsigned char* buf, int kb) {
+    if (kb + KT > k1) {
+      // What lies behind the keys may be anything; its weight is 0, and 0 times NaN is NaN.
+#pragma unroll
+      for (int i = 0; i < S::kLoads; ++i)
+        if (kb + my_row + i * S::kApart >= k1) vr[i] = u32x4{0, 0, 0, 0};
+    }
+    if (kb + KT - 1 > lim_block && causal) {
+      // Some row does not see some of these keys.  Their weight is 0 there, but its product with a value
+      // that is no number would be none either: such values are left out here and added at the end.
+      uint32_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < S::kLoads; ++i) odd |= drop_infinities<DT>(vr[i]);
+      if (odd) sh.odd_values[wk] = 1;
     }
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
       const int row = my_row + i * S::kApart;
       const int at = row * RB + ((my_piece ^ mix<RB>(row)) << 4);
-      *reinterpret_cast<u32x4*>(buf + at) = kr[i];
+      *reinterpret_cast<u32x4*>(buf + at) = my_on ? kr[i] : u32x4{0, 0, 0, 0};
       *reinterpret_cast<u32x4*>(buf + S::kTileBytes + at) = vr[i];
     }
   };
 
-  f32x16 o[QT][kDT];
-  float m[QT], l[QT];
+  acc o[kDT];
+  float m = kLowest, l = 0.f;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    m[t] = kLowest;
-    l[t] = 0.f;
-#pragma unroll
-    for (int i = 0; i < kDT; ++i) o[t][i] = f32x16{};
+  for (int i = 0; i < kDT; ++i) o[i] = acc{};
+  if (threadIdx.x < WK) sh.odd_values[threadIdx.x] = 0;
+  if (steps > 0) {
+    load_tile(kfirst);
+    load_pages(kfirst + kstep);
   }
-
-  if (threadIdx.x < 4) odd_values[threadIdx.x] = 0;
-  const int steps = (k1 - k0 + KT * WK - 1) / (KT * WK);
-  const int kstep = KT * WK, kfirst = k0 + wk * KT;
-  load_pages(kfirst);
-  load_tile(kfirst);
-  load_pages(kfirst + kstep);
   __syncthreads();
 
   for (int it = 0; it < steps; ++it) {
     const int kb = kfirst + it * kstep;
     unsigned char* buf = my_lds + (S::kBuffers > 1 ? (it & 1) * 2 * S::kTileBytes : 0);
     if (S::kBuffers == 1) __builtin_amdgcn_wave_barrier();
-    store_tile(buf, kb, it);
+    store_tile(buf, kb);
     load_tile(kb + kstep);
     load_pages(kb + 2 * kstep);
-    if (WM > 1) {
-      __syncthreads();
-      if (causal && threadIdx.x == 0) odd_values[(it + 3) & 3] = 0;  // the last step's, used again three steps on
-    } else {
-      __builtin_amdgcn_wave_barrier();
-    }
-    const bool odd = causal && kb + KT - 1 > lim_block && *(volatile int*)&odd_values[(WM > 1 ? it : wk) & 3] != 0;
+    if (WM > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
     const unsigned char* kl = buf;
     const unsigned char* vl = buf + S::kTileBytes;
 #pragma unroll
     for (int sub = 0; sub < kSub; ++sub) {
-      f32x16 sc[QT];
+      float sc[M::kScores];
 #pragma unroll
-      for (int t = 0; t < QT; ++t) sc[t] = f32x16{};
-      const int krow = sub * 32 + col;
+      for (int t = 0; t < M::kTiles; ++t) {
+        const int krow = sub * 32 + t * QW + col;
+        acc x = acc{};
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const int at = krow * RB + ((M::piece(s, half) ^ mix<RB>(krow)) << 4);
-        const QFrag kf = *reinterpret_cast<const QFrag*>(kl + at);
+        for (int s = 0; s < kSteps; ++s)
+          x = M::qk(*reinterpret_cast<const u32x4*>(kl + krow * RB + (((M::kGroups * s + grp) ^ mix<RB>(krow)) << 4)), q[s], x);
 #pragma unroll
-        for (int t = 0; t < QT; ++t) sc[t] = M::qk(kf, q[t][s], sc[t]);
+        for (int i = 0; i < M::kRegs; ++i) sc[t * M::kRegs + i] = x[i];
       }
       const int first = kb + sub * 32;
       if (first + 31 > lim_first) {
 #pragma unroll
-        for (int t = 0; t < QT; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = first + 8 * (i / 4) + 4 * half + i % 4;
-            sc[t][i] = key <= lim[t] ? sc[t][i] : -INFINITY;
-          }
+        for (int u = 0; u < M::kScores; ++u) sc[u] = first + M::place(u, grp) <= lim ? sc[u] : -INFINITY;
       }
+      float top = sc[0];
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        float top = sc[t][0];
+      for (int u = 1; u < M::kScores; ++u) top = fmaxf(top, sc[u]);
+      top = groups_max<QW>(top) * scale2;
+      // The reference of the exponentials follows the maximum only where it has grown by more than a factor
+      // of 2^6: until then the weights are at most 64, and nothing is rescaled.
+      if (__any(top > m + 6.f)) {
+        const float now = fmaxf(m, top);
+        const float keep = __builtin_amdgcn_exp2f(m - now);
+        m = now;
+        l *= keep;
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[t][i]);
-        top = other_half_max(top) * scale2;
-        // The reference of the exponentials follows the maximum only where it has grown by more than a factor
-        // of 2^6: until then the weights are at most 64, and nothing is rescaled.
-        if (__any(top > m[t] + 6.f)) {
-          const float now = fmaxf(m[t], top);
-          const float keep = __builtin_amdgcn_exp2f(m[t] - now);
-          m[t] = now;
-          l[t] *= keep;
-#pragma unroll
-          for (int i = 0; i < kDT; ++i) o[t][i] *= keep;
-        }
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          sc[t][i] = __builtin_amdgcn_exp2f(fmaf(sc[t][i], scale2, -m[t]));
-          sum += sc[t][i];
-        }
-        l[t] += sum;
+        for (int i = 0; i < kDT; ++i) o[i] *= keep;
       }
-      if (__builtin_expect(odd, 0)) {
-#pragma unroll 1
-        for (int kk = 0; kk < 32; ++kk) {
-          const int row = sub * 32 + kk;
+      float sum = 0.f;
 #pragma unroll
-          for (int t = 0; t < QT; ++t) {
-            float w = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) w = 8 * (i / 4) + i % 4 == (kk & ~4) ? sc[t][i] : w;
-            w = __shfl(w, col + 32 * ((kk >> 2) & 1));
-            if (DT == kBF16) w = bf16_lo(bf16_pair(w, 0.f));
-            const bool seen = first + kk <= lim[t];
-#pragma unroll
-            for (int i = 0; i < kDT; ++i)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const int e = i * 32 + 8 * j + 4 * half;
-                const int at = row * RB + (((e / M::kVec) ^ mix<RB>(row)) << 4) + (e % M::kVec) * S::kEsz;
-                Piece<DT, 4> v;
-                __builtin_memcpy(&v, __builtin_assume_aligned(vl + at, sizeof v), sizeof v);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) o[t][i][4 * j + k] = seen ? fmaf(w, v.get(k), o[t][i][4 * j + k]) : o[t][i][4 * j + k];
-              }
-          }
-        }
-        continue;
+      for (int u = 0; u < M::kScores; ++u) {
+        sc[u] = __builtin_amdgcn_exp2f(fmaf(sc[u], scale2, -m));
+        sum += sc[u];
       }
+      l += sum;
       if constexpr (DT == kBF16) {
-        bf16x8 p[QT][2];
+        // values: four keys at a lane's column of 16, by the transposing read of 16 lanes
+        const int vrow = 4 * grp + ((lane & 15) >> 2);
 #pragma unroll
-        for (int t = 0; t < QT; ++t)
+        for (int s = 0; s < M::kScores / 8; ++s) {
+          u32x4 p;
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            u32x4 w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = bf16_pair(sc[t][8 * s + 2 * i], sc[t][8 * s + 2 * i + 1]);
-            p[t][s] = __builtin_bit_cast(bf16x8, w);
-          }
-        // values: four keys at a lane's column of 32, by the transposing read of 16 lanes
-        const int vrow = 4 * half + ((lane & 15) >> 2);
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
+          for (int i = 0; i < 4; ++i) p[i] = bf16_pair(sc[8 * s + 2 * i], sc[8 * s + 2 * i + 1]);
 #pragma unroll
           for (int i = 0; i < kDT; ++i) {
-            bf16x8 vf;
-            i16x4 part[2];
+            uint2 part[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              const int row = sub * 32 + 16 * s + 8 * j + vrow;
-              const int piece = i * 4 + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+              const int row = sub * 32 + M::kRun * (2 * s + j) + vrow;
+              const int piece = i * (QW / 8) + (QW == 32 ? 2 * ((lane >> 4) & 1) : 0) + ((lane >> 1) & 1);
               const int at = row * RB + ((piece ^ mix<RB>(row)) << 4) + 8 * (lane & 1);
-              part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (__attribute__((address_space(3))) i16x4*)(vl + at));
+              part[j] = __builtin_bit_cast(
+                  uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(vl + at)));
             }
-            const u32x4 both = {__builtin_bit_cast(uint2, part[0]).x, __builtin_bit_cast(uint2, part[0]).y,
-                                __builtin_bit_cast(uint2, part[1]).x, __builtin_bit_cast(uint2, part[1]).y};
-            vf = __builtin_bit_cast(bf16x8, both);
-#pragma unroll
-            for (int t = 0; t < QT; ++t) o[t][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[t][s], o[t][i], 0, 0, 0);
+            o[i] = M::pv(u32x4{part[0].x, part[0].y, part[1].x, part[1].y}, p, o[i]);
           }
+        }
       } else {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int row = sub * 32 + 8 * (j / 4) + 4 * half + j % 4;
+        for (int u = 0; u < M::kScores; ++u) {
+          const int row = sub * 32 + M::place(u, grp);
 #pragma unroll
           for (int i = 0; i < kDT; ++i) {
-            const int at = row * RB + (((i * 8 + (col >> 2)) ^ mix<RB>(row)) << 4) + 4 * (col & 3);
-            const float vf = *reinterpret_cast<const float*>(vl + at);
-#pragma unroll
-            for (int t = 0; t < QT; ++t) o[t][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, sc[t][j], o[t][i], 0, 0, 0);
+            const int at = row * RB + (((i * (QW / 4) + (col >> 2)) ^ mix<RB>(row)) << 4) + 4 * (col & 3);
+            o[i] = M::av(*reinterpret_cast<const float*>(vl + at), sc[u], o[i]);
           }
         }
       }
     }
   }
   if (bad_page) flag(c, kBadPage);
+  if (causal) {
+    if (WM > 1) __syncthreads();
+    if (*(volatile int*)&sh.odd_values[wk] != 0) {
+      // Values that are no numbers, key by key, for the rows that see them.
+#pragma unroll 1
+      for (int it = 0; it < steps * KT; ++it) {
+        const int kb = kfirst + it / KT * kstep, key = kb + it % KT;
+        if (kb + KT - 1 <= lim_block || key >= k1) continue;
+        bool bad;
+        const long at = key_offset(c, table, key, bad) + (long)head * c.head_ld;
+        float w = 0.f;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) l[t] = other_half_sum(l[t]);
-
-  const long all = (long)c.T * c.Hq;
-  if constexpr (WK == 1) {
+        for (int s = 0; s < kSteps; ++s) {
+          const int e = (M::kGroups * s + grp) * M::kVec;
+          Piece<DT, M::kVec> kf = {}, qf;
+          if (e < c.d) kf = load_piece<DT, M::kVec>(a.k_pool, at + e);
+          __builtin_memcpy(&qf, &q[s], 16);
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      if (tok[t] < 0) continue;
-      const long id = (long)tok[t] * c.Hq + qh[t];
-      if (sp.parts > 1) {
-        const long at = (sp.first_part + blockIdx.z) * all + id;
-        if (half == 0) sp.part_ml[at] = make_float2(m[t], l[t]);
+          for (int j = 0; j < M::kVec; ++j) w = fmaf(qf.get(j), kf.get(j), w);
+        }
+        w = __builtin_amdgcn_exp2f(fmaf(groups_sum<QW>(w), scale2, -m));
+        if (key > lim) continue;
 #pragma unroll
         for (int i = 0; i < kDT; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int e = i * 32 + 8 * j + 4 * half;
-            if (e < c.d)
-              *reinterpret_cast<f32x4v*>(sp.part_o + at * c.d + e) =
-                  f32x4v{o[t][i][4 * j], o[t][i][4 * j + 1], o[t][i][4 * j + 2], o[t][i][4 * j + 3]};
+          for (int j = 0; j < M::kRegs / 4; ++j) {
+            const int e = min(i * QW + M::place(4 * j, grp), c.d - 4);  // (past the head: results that are not stored)
+            const Piece<DT, 4> v = load_piece<DT, 4>(a.v_pool, at + e);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (!(fabsf(v.get(k)) < INFINITY)) o[i][4 * j + k] = fmaf(w, v.get(k), o[i][4 * j + k]);
           }
-        continue;
       }
-      const float inv = l[t] == 0.f ? 0.f : 1.f / l[t];
-      if (a.lse != nullptr && half == 0) a.lse[id] = l[t] == 0.f ? -INFINITY : (m[t] + log2f(l[t])) * kLn2;
-      const long at = (long)tok[t] * a.out_ld + (long)qh[t] * c.d;
+    }
+  }
+  l = groups_sum<QW>(l);
+
+  const long all = (long)c.T * c.Hq;
+  if constexpr (WK == 1) {
+    if (!in) return;
+    const long id = (long)(tok0 + my_tok) * c.Hq + qh;
+    if (sp.parts > 1) {
+      const long at = (sp.first_part + part) * all + id;
+      if (grp == 0) sp.part_ml[at] = make_float2(m, l);
 #pragma unroll
       for (int i = 0; i < kDT; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int e = i * 32 + 8 * j + 4 * half;
-          if (e >= c.d) continue;
-          float x[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) x[k] = o[t][i][4 * j + k] * inv;
-          store_piece<DT, 4>(a.out, at + e, round_piece<DT, 4>(x));
+        for (int j = 0; j < M::kRegs / 4; ++j) {
+          const int e = i * QW + M::place(4 * j, grp);
+          if (e < c.d)
+            *reinterpret_cast<f32x4v*>(sp.part_o + at * c.d + e) = f32x4v{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
         }
+      return;
     }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (a.lse != nullptr && grp == 0) a.lse[id] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    const long at = (long)(tok0 + my_tok) * a.out_ld + (long)qh * c.d;
+#pragma unroll
+    for (int i = 0; i < kDT; ++i)
+#pragma unroll
+      for (int j = 0; j < M::kRegs / 4; ++j) {
+        const int e = i * QW + M::place(4 * j, grp);
+        if (e >= c.d) continue;
+        float x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = o[i][4 * j + k] * inv;
+        store_piece<DT, 4>(a.out, at + e, round_piece<DT, 4>(x));
+      }
   } else {
     // The key groups' results are joined in LDS, in the tiles' place.
-    if (half == 0) joined[wk][col] = make_float2(m[0], l[0]);
+    if (grp == 0) sh.joined[wk][col] = make_float2(m, l);
     __syncthreads();
     float top = kLowest, total = 0.f;
 #pragma unroll
-    for (int w = 0; w < WK; ++w) top = fmaxf(top, joined[w][col].x);
+    for (int w = 0; w < WK; ++w) top = fmaxf(top, sh.joined[w][col].x);
 #pragma unroll
-    for (int w = 0; w < WK; ++w) total += joined[w][col].y * __builtin_amdgcn_exp2f(joined[w][col].x - top);
-    const float mine = __builtin_amdgcn_exp2f(m[0] - top);
+    for (int w = 0; w < WK; ++w) total += sh.joined[w][col].y * __builtin_amdgcn_exp2f(sh.joined[w][col].x - top);
+    const float keep = __builtin_amdgcn_exp2f(m - top);
     float* mat = reinterpret_cast<float*>(my_lds);
 #pragma unroll
     for (int i = 0; i < kDT; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int piece = i * 8 + 2 * j + half;  // (of four elements)
+      for (int j = 0; j < M::kRegs / 4; ++j) {
+        const int piece = (i * QW + M::place(4 * j, grp)) / 4;
         *reinterpret_cast<f32x4v*>(mat + col * DP + ((piece ^ (col & 7)) << 2)) =
-            f32x4v{o[0][i][4 * j] * mine, o[0][i][4 * j + 1] * mine, o[0][i][4 * j + 2] * mine, o[0][i][4 * j + 3] * mine};
+            f32x4v{o[i][4 * j] * keep, o[i][4 * j + 1] * keep, o[i][4 * j + 2] * keep, o[i][4 * j + 3] * keep};
       }
-    if (wk == 0 && half == 0) joined[WK][col] = make_float2(top, total);
+    if (wk == 0 && grp == 0) sh.joined[4][col] = make_float2(top, total);
     __syncthreads();
     constexpr int kQuads = DP / 4;
-    for (int e = threadIdx.x; e < 32 * kQuads; e += S::kThreads) {
+    for (int e = threadIdx.x; e < QW * kQuads; e += S::kThreads) {
       const int rr = e / kQuads, piece = e % kQuads, row = row0 + rr;
-      if (row >= tl.rows || piece * 4 >= c.d) continue;
+      if (row >= rows || piece * 4 >= c.d) continue;
       f32x4v x = {};
 #pragma unroll
       for (int w = 0; w < WK; ++w)
         x += *reinterpret_cast<const f32x4v*>(reinterpret_cast<const float*>(lds + w * (S::kBuffers * 2 * S::kTileBytes)) + rr * DP +
                                               ((piece ^ (rr & 7)) << 2));
-      const int i = row / r, h = head * r + row - i * r;
-      const long id = (long)(tl.tok0 + i) * c.Hq + h;
-      const float2 ml = joined[WK][rr];
+      const int i = token_in(a, row), h = head * r + row - i * r;
+      const long id = (long)(tok0 + i) * c.Hq + h;
+      const float2 ml = sh.joined[4][rr];
       if (sp.parts > 1) {
-        const long at = (sp.first_part + blockIdx.z) * all + id;
+        const long at = (sp.first_part + part) * all + id;
         if (piece == 0) sp.part_ml[at] = ml;
         *reinterpret_cast<f32x4v*>(sp.part_o + at * c.d + piece * 4) = x;
         continue;
@@ -525,9 +514,29 @@ __global__ __launch_bounds__(64 * WM * WK) void k_attend(Attend a, Cache c, Part
       const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
       if (a.lse != nullptr && piece == 0) a.lse[id] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
       const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
-      store_piece<DT, 4>(a.out, (long)(tl.tok0 + i) * a.out_ld + (long)h * c.d + piece * 4, round_piece<DT, 4>(y));
+      store_piece<DT, 4>(a.out, (long)(tok0 + i) * a.out_ld + (long)h * c.d + piece * 4, round_piece<DT, 4>(y));
     }
   }
+}
+
+// Block number -> (row tile, head, part): the pairs of a head and a part fastest, so that the blocks that
+// read the same keys lie on the same die wherever the pairs are a multiple of eight; the tiles that see
+// most keys first.
+__device__ __forceinline__ void attend_place(const Cache& c, const Parting& sp, unsigned id, long& slot, int& head, int& part) {
+  const unsigned pairs = (unsigned)c.Hkv * (unsigned)sp.chunks, s = id / pairs, p = id - s * pairs;
+  part = (int)(p / (unsigned)c.Hkv);
+  head = (int)(p - (unsigned)part * (unsigned)c.Hkv);
+  slot = sp.slots - 1 - (long)s;
+}
+
+template <int DT, int DP, int QW, int WM, int WK, int KT>
+__global__ __launch_bounds__(64 * WM * WK, DT == kBF16 && DP <= 128 ? 2 : 1) void k_attend(Attend a, Cache c, Parting sp) {
+  extern __shared__ __align__(16) unsigned char lds[];
+  __shared__ AttendShared sh;
+  long slot;
+  int head, part;
+  attend_place(c, sp, blockIdx.x, slot, head, part);
+  attend_tile<DT, DP, QW, WM, WK, KT>(a, c, sp, lds, sh, slot, head, part);
 }
 
 // Joins a row's parts: 2^lanes_shift lanes per row, four elements each.

@@ -173,7 +173,10 @@ def attend(c, *, scale, causal=True, want_lse=True, status=None, ws_fill=None, o
     width = c.Hq * c.d
     room = torch.full((c.T, width + out_pad), 7.0, dtype=c.dtype, device="cuda")
     lse = torch.full((c.T, c.Hq), 7.0, device="cuda") if want_lse else None
-    D.dart_attend(cache, to_gpu(c.q), k_pool, v_pool, room[:, :width], ws, scale=scale, causal=causal, lse=lse,
+    q = to_gpu(c.q)
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())  # for what the lines above write
+    D.dart_attend(cache, q, k_pool, v_pool, room[:, :width], ws, scale=scale, causal=causal, lse=lse,
                   status=status, stream=stream)
     torch.cuda.synchronize()
     assert bool((room[:, width:] == 7.0).all())
