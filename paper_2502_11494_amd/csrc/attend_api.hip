@@ -19,6 +19,8 @@ constexpr int64_t kMaxLd = int64_t(1) << 24;       // row strides of q, k, v and
 constexpr int64_t kMaxPoolLd = int64_t(1) << 40;   // strides inside the pools, elements
 constexpr int kMaxSequences = 1 << 20, kMaxTokens = 1 << 24, kMaxKeys = 1 << 27, kMaxPage = 1 << 20;
 constexpr int kMaxHeads = 1024, kMaxHead = 256;
+constexpr long kJoinSets = 1L << 15;  // sets of lanes of a join that fill the chip
+constexpr long kMaxJoined = 1L << 24;  // (token, query head) pairs whose parts are joined
 constexpr long kMaxRows = 1L << 28, kMaxBlocks = (1L << 23) - 1;  // (token, head) pairs of a key head; blocks of a launch
 
 inline bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
@@ -167,16 +169,17 @@ dart_status set_rows(Rotate& a, int dtype, int T, const void* q, int64_t q_ld, c
 }
 
 // ---- attention: which tiles, how many parts ---------------------------------------------------
-enum Kind { kFew, kMany, kWide };  // 16 rows, the keys dealt to four waves; 128 rows; 256 rows
+enum Kind { kFew, kMany, kWide };  // 16 rows, the keys dealt to four waves; four waves of rows; eight
 
 struct AttendPlan {
   Kind own_kind, pre_kind;
   Parting own, pre;
+  bool both;  // one launch takes the prefixes and the own keys
   int parts;
   size_t o_ml, total;
 };
 
-int rows_of(Kind k) { return k == kFew ? 16 : k == kMany ? 128 : 256; }
+int rows_of(Kind k, int dtype, int d) { return k == kFew ? 16 : k == kWide ? 256 : 4 * many_columns(dtype == DART_BF16 ? kBF16 : kF32, d); }
 long blocks_of(const Cache& c, const Parting& p) { return p.slots * c.Hkv * p.chunks; }
 
 // rows: (token, head) pairs of a sequence or group at most; owners: how many of them.
@@ -186,7 +189,7 @@ Kind plan_parting(const Cache& c, int dtype, bool prefix, long rows, int owners,
   const bool wide = dtype == DART_BF16 && c.d <= 128 && ((long)c.T * r / 256) * c.Hkv >= 512;
   Kind kind = rows <= 32 ? kFew : wide && rows > 128 ? kWide : kMany;
   if (dtype == DART_F32 && c.d > 128) kind = kMany;
-  const int bm = rows_of(kind);
+  const int bm = rows_of(kind, dtype, c.d);
   p = {};
   p.prefix = prefix;
   p.few = kind == kFew;
@@ -197,8 +200,11 @@ Kind plan_parting(const Cache& c, int dtype, bool prefix, long rows, int owners,
     p.slots = (long)c.T * r / bm + owners;
   }
   const long blocks = std::max(1L, std::min(p.slots, (long)owners * ((rows + bm - 1) / bm)) * c.Hkv);
-  // enough parts to fill the chip twice, of 256 keys at least
-  const long want = std::max(1L, 512 / blocks);
+  // Parts until every compute unit has a block, of 256 keys at least; more cost their start (7 us a round) and the
+  // join: 64 rows of 28 + 4 heads over 8000 keys 197 us in one part, 40 in 128 blocks, 31 in 256, 33 in 512, 46 in
+  // 1024; 64 answers over one prefix of 9216 229, 43, 34, 42 and 48.  32-bit tiles of four waves are bound by the
+  // matrix cores' latency and want company: 637 causal tokens of 32 heads 69 us in 320 blocks, 58 in 960.
+  const long want = std::max(1L, (dtype == DART_F32 && kind == kMany ? 1024 : 256) / blocks);
   const long chunk = std::max(256L, ((max_keys + want - 1) / want + 255) / 256 * 256);
   p.chunk = (int)chunk;
   p.chunks = std::max(1, (int)((max_keys + chunk - 1) / chunk));
@@ -216,8 +222,10 @@ dart_status plan_attend(const Cache& c, int dtype, AttendPlan& p) {
     p.pre_kind = plan_parting(c, dtype, true, std::max(1L, (rows + c.groups - 1) / c.groups), c.groups, c.max_prefix, p.pre);
     p.parts += p.pre.chunks;
     p.own.first_part = p.pre.chunks;
+    p.both = p.own_kind != kWide && p.pre_kind != kWide && (dtype == DART_BF16 || c.d <= 128);
   }
-  if (blocks_of(c, p.own) > kMaxBlocks || blocks_of(c, p.pre) > kMaxBlocks) return DART_ERR_SHAPE;
+  if (blocks_of(c, p.own) + blocks_of(c, p.pre) > kMaxBlocks) return DART_ERR_SHAPE;
+  if (p.parts > 1 && (long)c.T * c.Hq > kMaxJoined) return DART_ERR_SHAPE;
   p.own.parts = p.pre.parts = p.parts;
   auto up = [](size_t v) { return (v + kAlign - 1) / kAlign * kAlign; };
   const size_t rows = (size_t)c.T * c.Hq;
@@ -241,14 +249,22 @@ dart_status launch_bf16(const Attend& a, const Cache& c, const Parting& sp, Kind
   if (kind == kFew) return launch_tiles<kBF16, DP, 16, 1, 4, 32>(a, c, sp, st);
   if constexpr (DP <= 128)
     if (kind == kWide) return launch_tiles<kBF16, DP, 32, 8, 1, 64>(a, c, sp, st);
-  return launch_tiles<kBF16, DP, 32, 4, 1, 64>(a, c, sp, st);
+  return launch_tiles<kBF16, DP, many_columns(kBF16, DP), 4, 1, 64>(a, c, sp, st);
 }
 
 template <int DP>
 dart_status launch_f32(const Attend& a, const Cache& c, const Parting& sp, Kind kind, hipStream_t st) {
   if constexpr (DP <= 128)
     if (kind == kFew) return launch_tiles<kF32, DP, 16, 1, 4, 32>(a, c, sp, st);
-  return launch_tiles<kF32, DP, 32, 4, 1, 32>(a, c, sp, st);
+  return launch_tiles<kF32, DP, many_columns(kF32, DP), 4, 1, 32>(a, c, sp, st);
+}
+
+template <int DT, int DP, int KT>
+dart_status launch_both(const Attend& a, const Cache& c, const Parting& pre, const Parting& own, hipStream_t st) {
+  constexpr int kLds = std::max(AttendShape<DT, DP, 16, 1, 4, 32>::kLds, AttendShape<DT, DP, many_columns(DT, DP), 4, 1, KT>::kLds);
+  const long n = blocks_of(c, pre);
+  k_attend_both<DT, DP, KT><<<dim3((unsigned)(n + blocks_of(c, own))), dim3(256), kLds, st>>>(a, c, pre, own, (unsigned)n);
+  return launched();
 }
 
 dart_status launch_attend(const Attend& a, const Cache& c, int dtype, const Parting& sp, Kind k, hipStream_t st) {
@@ -327,18 +343,30 @@ dart_status dart_attend(const dart_cache* cache, const void* q, int64_t q_ld, co
   float2* part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(ws) + p.o_ml);
   p.own.part_o = p.pre.part_o = part_o;
   p.own.part_ml = p.pre.part_ml = part_ml;
-  if (c.groups > 0) DART_TRY(launch_attend(a, c, cache->dtype, p.pre, p.pre_kind, st));
-  DART_TRY(launch_attend(a, c, cache->dtype, p.own, p.own_kind, st));
+  const bool bf16 = cache->dtype == DART_BF16;
+  if (p.both && bf16) {
+    DART_TRY(c.d <= 64    ? (launch_both<kBF16, 64, 64>(a, c, p.pre, p.own, st))
+             : c.d <= 128 ? (launch_both<kBF16, 128, 64>(a, c, p.pre, p.own, st))
+                          : (launch_both<kBF16, 256, 64>(a, c, p.pre, p.own, st)));
+  } else if (p.both) {
+    DART_TRY(c.d <= 64 ? (launch_both<kF32, 64, 32>(a, c, p.pre, p.own, st)) : (launch_both<kF32, 128, 32>(a, c, p.pre, p.own, st)));
+  } else {
+    if (c.groups > 0) DART_TRY(launch_attend(a, c, cache->dtype, p.pre, p.pre_kind, st));
+    DART_TRY(launch_attend(a, c, cache->dtype, p.own, p.own_kind, st));
+  }
   if (p.parts == 1) return DART_OK;
-  int lanes_shift = 0;
+  int lanes_shift = 0, split_shift = 0;
   while ((4 << lanes_shift) < c.d) ++lanes_shift;
-  const long per_block = 4L << (6 - lanes_shift), blocks = ((long)c.T * c.Hq + per_block - 1) / per_block;
-  if (cache->dtype == DART_BF16)
+  // many parts of few rows are shared by up to a block's sets of lanes, four parts at least to each
+  while (split_shift < 8 - lanes_shift && (4 << split_shift) < p.parts && ((long)c.T * c.Hq << split_shift) < kJoinSets) ++split_shift;
+  const int rows_shift = 8 - lanes_shift - split_shift;
+  const long blocks = (((long)c.T * c.Hq - 1) >> rows_shift) + 1;
+  if (bf16)
     k_attend_join<kBF16><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, part_o, part_ml,
-                                                                      lanes_shift);
+                                                                      lanes_shift, split_shift);
   else
     k_attend_join<kF32><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, part_o, part_ml,
-                                                                     lanes_shift);
+                                                                     lanes_shift, split_shift);
   return launched();
 }
 

@@ -43,23 +43,21 @@ struct Seq {
   bool valid;
 };
 
-__device__ __forceinline__ Seq sequence_of(const Cache& c, int b) {
+__device__ __forceinline__ Seq make_sequence(const Cache& c, int lo, int hi, int kv) {
   Seq s;
-  if (c.cu == nullptr) {
-    s.tok0 = b;
-    s.n = 1;
-    s.valid = true;
-  } else {
-    const int lo = c.cu[b], hi = c.cu[b + 1];
-    s.valid = lo >= 0 && hi >= lo && hi <= c.T && hi - lo <= c.max_q;
-    s.tok0 = lo < 0 ? 0 : lo < c.T ? lo : c.T;
-    s.n = (hi < c.T ? hi : c.T) - s.tok0;
-    if (s.n < 0) s.n = 0;
-  }
-  s.kv = c.kv_len[b];
-  if (s.kv < 0 || s.kv > c.max_kv || (long)s.kv > ((long)c.pages_ld << c.page_shift)) s.valid = false;
+  s.valid = lo >= 0 && hi >= lo && hi <= c.T && hi - lo <= c.max_q;
+  s.tok0 = lo < 0 ? 0 : lo < c.T ? lo : c.T;
+  s.n = (hi < c.T ? hi : c.T) - s.tok0;
+  if (s.n < 0) s.n = 0;
+  s.kv = kv;
+  if (kv < 0 || kv > c.max_kv || (long)kv > ((long)c.pages_ld << c.page_shift)) s.valid = false;
   if (!s.valid) s.kv = 0;
   return s;
+}
+
+__device__ __forceinline__ Seq sequence_of(const Cache& c, int b) {
+  const bool one = c.cu == nullptr;  // a token each
+  return make_sequence(c, one ? b : c.cu[b], one ? b + 1 : c.cu[b + 1], c.kv_len[b]);
 }
 
 // Keys of group g's prefix; -1 if its length or its sequences are not as they have to be.

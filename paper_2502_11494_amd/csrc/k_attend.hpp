@@ -178,6 +178,10 @@ struct AttendShape {
   static_assert(WK == 1 || QW * DP * 4 <= kBuffers * 2 * kTileBytes, "joined in the tiles' place");
 };
 
+// Columns of a wave's tile where four waves take the rows: 32 halve what LDS has to deliver per product, but with
+// 32-bit rows the matrix cores are what counts, and with heads over 128 the registers are.
+constexpr int many_columns(int dt, int d) { return dt == kBF16 && d <= 128 ? 32 : 16; }
+
 // What a block keeps in LDS beside the tiles.
 struct AttendShared {
   int odd_values[4];
@@ -211,8 +215,21 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     table = c.prefix_pages + (long)g * c.prefix_ld;
     tile = (int)(slot - ((long)tok0 * r / S::kBM + g));
   } else {
-    const int b = sp.per_owner ? (int)slot / sp.per_owner : slot_owner<S::kBM>(c, nullptr, c.B, r, slot);
-    const Seq s = sequence_of(c, b);
+    int b;
+    Seq s;
+    if (sp.per_owner) {
+      b = (int)slot / sp.per_owner;
+      s = sequence_of(c, b);
+    } else if (c.B <= kWave) {  // (all sequences in one look: the loads do not wait for one another)
+      const int i = lane < c.B ? lane : c.B - 1, lo = c.cu[i], hi = c.cu[i + 1], keys = c.kv_len[i];
+      const unsigned long long low =
+          __ballot(lane < c.B && (long)(lo < 0 ? 0 : lo < c.T ? lo : c.T) * r / S::kBM + lane <= slot);
+      b = low ? 63 - __builtin_clzll(low) : 0;
+      s = make_sequence(c, __builtin_amdgcn_readlane(lo, b), __builtin_amdgcn_readlane(hi, b), __builtin_amdgcn_readlane(keys, b));
+    } else {
+      b = slot_owner<S::kBM>(c, nullptr, c.B, r, slot);
+      s = sequence_of(c, b);
+    }
     if (!s.valid && threadIdx.x == 0) flag(c, kBadSequence);
     tok0 = s.tok0;
     n = s.n;
@@ -307,7 +324,21 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     }
   };
 
+  // This lane's share of its query's result, four elements of the head at a time: quad number x is elements
+  // quad_at(x) .. + 3.
   acc o[kDT];
+  constexpr int kQuads = kDT * M::kRegs / 4;
+  auto quad_at = [&](int x) {
+    if (DT == kBF16) return x / (M::kRegs / 4) * QW + M::place(4 * (x % (M::kRegs / 4)), grp);
+    return 4 * (x / M::kRegs * QW + M::place(x % M::kRegs, grp));
+  };
+  auto quad = [&](int x) {
+    f32x4v v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      v[k] = DT == kBF16 ? o[x / (M::kRegs / 4)][4 * (x % (M::kRegs / 4)) + k] : o[(4 * (x / M::kRegs) + k) % kDT][x % M::kRegs];
+    return v;
+  };
   float m = kLowest, l = 0.f;
 #pragma unroll
   for (int i = 0; i < kDT; ++i) o[i] = acc{};
@@ -391,13 +422,15 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
           }
         }
       } else {
+        // (a lane's 16 bytes feed four result tiles, whose rows are therefore every fourth element of the head)
 #pragma unroll
         for (int u = 0; u < M::kScores; ++u) {
           const int row = sub * 32 + M::place(u, grp);
 #pragma unroll
-          for (int i = 0; i < kDT; ++i) {
-            const int at = row * RB + (((i * (QW / 4) + (col >> 2)) ^ mix<RB>(row)) << 4) + 4 * (col & 3);
-            o[i] = M::av(*reinterpret_cast<const float*>(vl + at), sc[u], o[i]);
+          for (int i = 0; i < kDT / 4; ++i) {
+            const f32x4v v = *reinterpret_cast<const f32x4v*>(vl + row * RB + (((i * QW + col) ^ mix<RB>(row)) << 4));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[4 * i + k] = M::av(v[k], sc[u], o[4 * i + k]);
           }
         }
       }
@@ -427,15 +460,15 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
         w = __builtin_amdgcn_exp2f(fmaf(groups_sum<QW>(w), scale2, -m));
         if (key > lim) continue;
 #pragma unroll
-        for (int i = 0; i < kDT; ++i)
+        for (int x = 0; x < kQuads; ++x) {
+          const Piece<DT, 4> v = load_piece<DT, 4>(a.v_pool, at + min(quad_at(x), c.d - 4));  // (past the head: not stored)
 #pragma unroll
-          for (int j = 0; j < M::kRegs / 4; ++j) {
-            const int e = min(i * QW + M::place(4 * j, grp), c.d - 4);  // (past the head: results that are not stored)
-            const Piece<DT, 4> v = load_piece<DT, 4>(a.v_pool, at + e);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (!(fabsf(v.get(k)) < INFINITY)) o[i][4 * j + k] = fmaf(w, v.get(k), o[i][4 * j + k]);
+          for (int k = 0; k < 4; ++k) {
+            if (fabsf(v.get(k)) < INFINITY) continue;
+            if constexpr (DT == kBF16) o[x / (M::kRegs / 4)][4 * (x % (M::kRegs / 4)) + k] += w * v.get(k);
+            else o[4 * (x / M::kRegs) + k][x % M::kRegs] += w * v.get(k);
           }
+        }
       }
     }
   }
@@ -449,29 +482,20 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
       const long at = (sp.first_part + part) * all + id;
       if (grp == 0) sp.part_ml[at] = make_float2(m, l);
 #pragma unroll
-      for (int i = 0; i < kDT; ++i)
-#pragma unroll
-        for (int j = 0; j < M::kRegs / 4; ++j) {
-          const int e = i * QW + M::place(4 * j, grp);
-          if (e < c.d)
-            *reinterpret_cast<f32x4v*>(sp.part_o + at * c.d + e) = f32x4v{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
-        }
+      for (int x = 0; x < kQuads; ++x)
+        if (quad_at(x) < c.d) *reinterpret_cast<f32x4v*>(sp.part_o + at * c.d + quad_at(x)) = quad(x);
       return;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     if (a.lse != nullptr && grp == 0) a.lse[id] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
     const long at = (long)(tok0 + my_tok) * a.out_ld + (long)qh * c.d;
 #pragma unroll
-    for (int i = 0; i < kDT; ++i)
-#pragma unroll
-      for (int j = 0; j < M::kRegs / 4; ++j) {
-        const int e = i * QW + M::place(4 * j, grp);
-        if (e >= c.d) continue;
-        float x[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = o[i][4 * j + k] * inv;
-        store_piece<DT, 4>(a.out, at + e, round_piece<DT, 4>(x));
-      }
+    for (int x = 0; x < kQuads; ++x) {
+      if (quad_at(x) >= c.d) continue;
+      const f32x4v v = quad(x) * inv;
+      const float y[4] = {v[0], v[1], v[2], v[3]};
+      store_piece<DT, 4>(a.out, at + quad_at(x), round_piece<DT, 4>(y));
+    }
   } else {
     // The key groups' results are joined in LDS, in the tiles' place.
     if (grp == 0) sh.joined[wk][col] = make_float2(m, l);
@@ -484,18 +508,13 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     const float keep = __builtin_amdgcn_exp2f(m - top);
     float* mat = reinterpret_cast<float*>(my_lds);
 #pragma unroll
-    for (int i = 0; i < kDT; ++i)
-#pragma unroll
-      for (int j = 0; j < M::kRegs / 4; ++j) {
-        const int piece = (i * QW + M::place(4 * j, grp)) / 4;
-        *reinterpret_cast<f32x4v*>(mat + col * DP + ((piece ^ (col & 7)) << 2)) =
-            f32x4v{o[i][4 * j] * keep, o[i][4 * j + 1] * keep, o[i][4 * j + 2] * keep, o[i][4 * j + 3] * keep};
-      }
+    for (int x = 0; x < kQuads; ++x)
+      *reinterpret_cast<f32x4v*>(mat + col * DP + ((quad_at(x) / 4 ^ (col & 7)) << 2)) = quad(x) * keep;
     if (wk == 0 && grp == 0) sh.joined[4][col] = make_float2(top, total);
     __syncthreads();
-    constexpr int kQuads = DP / 4;
-    for (int e = threadIdx.x; e < QW * kQuads; e += S::kThreads) {
-      const int rr = e / kQuads, piece = e % kQuads, row = row0 + rr;
+    constexpr int kRow = DP / 4;
+    for (int e = threadIdx.x; e < QW * kRow; e += S::kThreads) {
+      const int rr = e / kRow, piece = e % kRow, row = row0 + rr;
       if (row >= rows || piece * 4 >= c.d) continue;
       f32x4v x = {};
 #pragma unroll
@@ -530,7 +549,7 @@ __device__ __forceinline__ void attend_place(const Cache& c, const Parting& sp, 
 }
 
 template <int DT, int DP, int QW, int WM, int WK, int KT>
-__global__ __launch_bounds__(64 * WM * WK, DT == kBF16 && DP <= 128 ? 2 : 1) void k_attend(Attend a, Cache c, Parting sp) {
+__global__ __launch_bounds__(64 * WM * WK, DP <= 128 && (DT == kBF16 || WK == 1) ? 2 : 1) void k_attend(Attend a, Cache c, Parting sp) {
   extern __shared__ __align__(16) unsigned char lds[];
   __shared__ AttendShared sh;
   long slot;
@@ -539,26 +558,44 @@ __global__ __launch_bounds__(64 * WM * WK, DT == kBF16 && DP <= 128 ? 2 : 1) voi
   attend_tile<DT, DP, QW, WM, WK, KT>(a, c, sp, lds, sh, slot, head, part);
 }
 
-// Joins a row's parts: 2^lanes_shift lanes per row, four elements each.
+// Prefixes and own keys in one launch: the first blocks take the prefixes, the rest fill in beside them.
+template <int DT, int DP, int KT>
+__global__ __launch_bounds__(256, DT == kBF16 && DP <= 128 ? 2 : 1) void k_attend_both(Attend a, Cache c, Parting pre, Parting own,
+                                                                                       unsigned pre_blocks) {
+  extern __shared__ __align__(16) unsigned char lds[];
+  __shared__ AttendShared sh;
+  const bool first = blockIdx.x < pre_blocks;
+  const Parting sp = first ? pre : own;
+  long slot;
+  int head, part;
+  attend_place(c, sp, first ? blockIdx.x : blockIdx.x - pre_blocks, slot, head, part);
+  if (sp.few) attend_tile<DT, DP, 16, 1, 4, 32>(a, c, sp, lds, sh, slot, head, part);
+  else attend_tile<DT, DP, many_columns(DT, DP), 4, 1, KT>(a, c, sp, lds, sh, slot, head, part);
+}
+
+// Joins a row's parts.  2^lanes_shift lanes hold a row, four elements each; 2^split_shift such sets of a block
+// share one row's parts where there are many, and join through LDS.  Eight parts are asked for at once.
 template <int DT>
 __global__ __launch_bounds__(256) void k_attend_join(Attend a, Cache c, int pre_chunk, int pre_parts, int own_chunk, const float* part_o,
-                                                     const float2* part_ml, int lanes_shift) {
+                                                     const float2* part_ml, int lanes_shift, int split_shift) {
+  __shared__ f32x4v set_x[256];
+  __shared__ float2 set_ml[256];
   const long all = (long)c.T * c.Hq;
-  const int lane = threadIdx.x & 63;
-  const long first = ((long)blockIdx.x * 4 + (threadIdx.x >> 6)) << (6 - lanes_shift);
-  const long id = first + (lane >> lanes_shift);
-  const int t0 = (int)(first / c.Hq);
-  int b0 = 0;
-  if (c.cu != nullptr && first < all) b0 = owner_of(c.cu, c.B, t0);
-  if (id >= all) return;
-  const int t = (int)(id / c.Hq), h = (int)(id - (long)t * c.Hq);
-  int b = c.cu == nullptr ? t : b0;
-  if (c.cu != nullptr)
-    while (b + 1 < c.B && c.cu[b + 1] <= t) ++b;  // (a wave's rows are a few tokens')
+  const int lane = threadIdx.x & 63, set = threadIdx.x >> lanes_shift, sub = set & ((1 << split_shift) - 1);
+  const int rows_shift = 8 - lanes_shift - split_shift;  // rows of a block
+  const long first = (long)blockIdx.x << rows_shift;
+  int b = (int)(first / c.Hq);
+  if (c.cu != nullptr) b = owner_of(c.cu, c.B, b);
+  const long id = first + (set >> split_shift);
+  bool row = id < all;
+  const int t = row ? (int)(id / c.Hq) : 0, h = (int)((row ? id : 0) - (long)t * c.Hq);
+  if (c.cu == nullptr) b = t;
+  else
+    while (b + 1 < c.B && c.cu[b + 1] <= t) ++b;  // (a block's rows are a few tokens')
   const Seq s = sequence_of(c, b);
   int own = s.kv;
   if (a.causal && s.kv - s.n + (t - s.tok0) + 1 < own) own = s.kv - s.n + (t - s.tok0) + 1;
-  if (t < s.tok0 || t >= s.tok0 + s.n) return;  // no sequence's token
+  row = row && t >= s.tok0 && t < s.tok0 + s.n;  // (else no sequence's token)
   int prefix = 0;
   if (c.groups > 0) {
     int g = 0, end = c.groups;
@@ -572,23 +609,57 @@ __global__ __launch_bounds__(256) void k_attend_join(Attend a, Cache c, int pre_
       prefix = own = 0;
     }
   }
-  if (!s.valid) prefix = own = 0;
+  if (!s.valid || !row) prefix = own = 0;
   const int np = prefix > 0 ? (prefix + pre_chunk - 1) / pre_chunk : 0;
-  const int no = own > 0 ? (own + own_chunk - 1) / own_chunk : 0;
+  const int n = np + (own > 0 ? (own + own_chunk - 1) / own_chunk : 0);
   const int e = (lane & ((1 << lanes_shift) - 1)) * 4;
   const bool in = e < c.d;
   float top = kLowest, l = 0.f;
   f32x4v x = {};
-  for (int i = 0; i < np + no; ++i) {
-    const long at = (i < np ? i : pre_parts + i - np) * all + id;
-    const float2 ml = part_ml[at];
-    const f32x4v y = in ? *reinterpret_cast<const f32x4v*>(part_o + at * c.d + e) : f32x4v{};
-    const float now = fmaxf(top, ml.x);
-    const float f = __builtin_amdgcn_exp2f(top - now), w = __builtin_amdgcn_exp2f(ml.x - now);
+  constexpr int kAtOnce = 8;
+  for (int i0 = sub; i0 < n; i0 += kAtOnce << split_shift) {
+    float2 ml[kAtOnce];
+    f32x4v y[kAtOnce];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      const int i = min(i0 + (j << split_shift), n - 1);  // (past the last: the last again, with no weight)
+      const long at = (i < np ? i : pre_parts + i - np) * all + id;
+      ml[j] = part_ml[at];
+      y[j] = *reinterpret_cast<const f32x4v*>(part_o + at * c.d + (in ? e : 0));
+    }
+    float now = top;
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) now = fmaxf(now, ml[j].x);
+    const float f = __builtin_amdgcn_exp2f(top - now);
     top = now;
-    l = l * f + ml.y * w;
-    x = x * f + y * w;
+    l *= f;
+    x *= f;
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      if (i0 + (j << split_shift) >= n) break;
+      const float w = __builtin_amdgcn_exp2f(ml[j].x - now);
+      l += ml[j].y * w;
+      x += y[j] * w;
+    }
   }
+  if (split_shift > 0) {
+    set_x[threadIdx.x] = x;
+    set_ml[threadIdx.x] = make_float2(top, l);
+    __syncthreads();
+    if (sub != 0) return;
+    const float mine = top;
+    for (int i = 1; i < 1 << split_shift; ++i) top = fmaxf(top, set_ml[threadIdx.x + (i << lanes_shift)].x);
+    const float f = __builtin_amdgcn_exp2f(mine - top);
+    l *= f;
+    x *= f;
+    for (int i = 1; i < 1 << split_shift; ++i) {
+      const float2 ml = set_ml[threadIdx.x + (i << lanes_shift)];
+      const float w = __builtin_amdgcn_exp2f(ml.x - top);
+      l += ml.y * w;
+      x += set_x[threadIdx.x + (i << lanes_shift)] * w;
+    }
+  }
+  if (!row) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if (a.lse != nullptr && e == 0) a.lse[id] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
   if (!in) return;
