@@ -434,8 +434,8 @@ typedef struct dart_cache {
   int32_t pages_ld;      /* entries of a row of `pages`, >= 1                                 */
   int32_t n_pages;       /* pages of the pools, >= 1                                          */
   int32_t page_size;     /* rows of a page: a power of two, 1..2^20                           */
-  int64_t page_ld, head_ld, row_ld; /* strides in elements: multiples of 8 (of 4 for 32-bit rows), row_ld >= d,
-                                       0 <= head_ld <= 2^40, 0 <= page_ld <= 2^40             */
+  int64_t page_ld, head_ld, row_ld; /* strides in elements: multiples of 8 (of 4 for 32-bit rows), d <= row_ld,
+                                       0 <= head_ld, 0 <= page_ld, none over 2^33             */
   int32_t groups;     /* shared prefixes, 0..B (0: none, the fields below are ignored)        */
   int32_t max_prefix; /* host-known upper bound of every prefix_len, 0..2^27                  */
   const int32_t* group_cu;     /* DEVICE int32[groups+1] from 0 to B                          */

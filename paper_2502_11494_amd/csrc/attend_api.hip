@@ -16,7 +16,7 @@ namespace {
 
 constexpr size_t kAlign = 256;
 constexpr int64_t kMaxLd = int64_t(1) << 24;       // row strides of q, k, v and outputs, elements
-constexpr int64_t kMaxPoolLd = int64_t(1) << 40;   // strides inside the pools, elements
+constexpr int64_t kMaxPoolLd = int64_t(1) << 33;   // strides inside the pools, elements: 16-byte units fit 32 bits
 constexpr int kMaxSequences = 1 << 20, kMaxTokens = 1 << 24, kMaxKeys = 1 << 27, kMaxPage = 1 << 20;
 constexpr int kMaxHeads = 1024, kMaxHead = 256;
 constexpr long kJoinSets = 1L << 15;  // sets of lanes of a join that fill the chip
@@ -79,6 +79,8 @@ dart_status make_cache(const dart_cache* u, Cache& c) {
   c.page_ld = u->page_ld;
   c.head_ld = u->head_ld;
   c.row_ld = u->row_ld;
+  c.page_16 = (uint32_t)(u->page_ld / a16);
+  c.row_16 = (uint32_t)(u->row_ld / a16);
   c.groups = u->groups;
   if (u->groups > 0) {
     if (u->max_prefix < 0 || u->max_prefix > kMaxKeys || u->prefix_ld < 1) return DART_ERR_SHAPE;

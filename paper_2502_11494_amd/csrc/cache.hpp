@@ -12,6 +12,7 @@ struct Cache {
   const int *cu, *kv_len, *pages;
   int pages_ld, n_pages, page_shift;
   long page_ld, head_ld, row_ld;  // elements
+  uint32_t page_16, row_16;       // the same strides in units of 16 bytes
   int groups, max_prefix, prefix_ld;
   const int *group_cu, *prefix_pages, *prefix_len;
   int* status;

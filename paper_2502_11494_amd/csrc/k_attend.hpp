@@ -268,8 +268,9 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     for (int i = 0; i < S::kLoads; ++i) {
       int page = pg[i];
       if ((unsigned)page >= (unsigned)c.n_pages) page = 0, bad_page = true;
-      const int row = min(kb + my_row + i * S::kApart, last_key) & row_mask;
-      const long off = ((long)page * c.page_ld + (long)row * c.row_ld) * S::kEsz;
+      const uint32_t row = min(kb + my_row + i * S::kApart, last_key) & row_mask;
+      // (32 by 32 bits: the wider products cost as much as a fifth of the step's exponentials)
+      const uint64_t off = ((uint64_t)(uint32_t)page * c.page_16 + (uint64_t)row * c.row_16) << 4;
       kr[i] = *reinterpret_cast<const u32x4*>(kp + off);
       vr[i] = *reinterpret_cast<const u32x4*>(vp + off);
     }
@@ -360,43 +361,47 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     else __builtin_amdgcn_wave_barrier();
     const unsigned char* kl = buf;
     const unsigned char* vl = buf + S::kTileBytes;
+    // scores of the step's keys: 32 at a time in sc[sub]
+    float sc[kSub][M::kScores];
+#pragma unroll
+    for (int t = 0; t < kSub * M::kTiles; ++t) {
+      const int krow = t * QW + col;
+      acc x = acc{};
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+        x = M::qk(*reinterpret_cast<const u32x4*>(kl + krow * RB + (((M::kGroups * s + grp) ^ mix<RB>(krow)) << 4)), q[s], x);
+#pragma unroll
+      for (int i = 0; i < M::kRegs; ++i) sc[t / M::kTiles][t % M::kTiles * M::kRegs + i] = x[i];
+    }
+    if (kb + KT - 1 > lim_first) {
+#pragma unroll
+      for (int sub = 0; sub < kSub; ++sub)
+#pragma unroll
+        for (int u = 0; u < M::kScores; ++u) sc[sub][u] = kb + sub * 32 + M::place(u, grp) <= lim ? sc[sub][u] : -INFINITY;
+    }
+    float top = sc[0][0];
+#pragma unroll
+    for (int sub = 0; sub < kSub; ++sub)
+#pragma unroll
+      for (int u = 0; u < M::kScores; ++u) top = fmaxf(top, sc[sub][u]);
+    top = groups_max<QW>(top) * scale2;
+    // The reference of the exponentials follows the maximum only where it has grown by more than a factor
+    // of 2^6: until then the weights are at most 64, and nothing is rescaled.
+    if (__any(top > m + 6.f)) {
+      const float now = fmaxf(m, top);
+      const float keep = __builtin_amdgcn_exp2f(m - now);
+      m = now;
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < kDT; ++i) o[i] *= keep;
+    }
 #pragma unroll
     for (int sub = 0; sub < kSub; ++sub) {
-      float sc[M::kScores];
-#pragma unroll
-      for (int t = 0; t < M::kTiles; ++t) {
-        const int krow = sub * 32 + t * QW + col;
-        acc x = acc{};
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s)
-          x = M::qk(*reinterpret_cast<const u32x4*>(kl + krow * RB + (((M::kGroups * s + grp) ^ mix<RB>(krow)) << 4)), q[s], x);
-#pragma unroll
-        for (int i = 0; i < M::kRegs; ++i) sc[t * M::kRegs + i] = x[i];
-      }
-      const int first = kb + sub * 32;
-      if (first + 31 > lim_first) {
-#pragma unroll
-        for (int u = 0; u < M::kScores; ++u) sc[u] = first + M::place(u, grp) <= lim ? sc[u] : -INFINITY;
-      }
-      float top = sc[0];
-#pragma unroll
-      for (int u = 1; u < M::kScores; ++u) top = fmaxf(top, sc[u]);
-      top = groups_max<QW>(top) * scale2;
-      // The reference of the exponentials follows the maximum only where it has grown by more than a factor
-      // of 2^6: until then the weights are at most 64, and nothing is rescaled.
-      if (__any(top > m + 6.f)) {
-        const float now = fmaxf(m, top);
-        const float keep = __builtin_amdgcn_exp2f(m - now);
-        m = now;
-        l *= keep;
-#pragma unroll
-        for (int i = 0; i < kDT; ++i) o[i] *= keep;
-      }
       float sum = 0.f;
 #pragma unroll
       for (int u = 0; u < M::kScores; ++u) {
-        sc[u] = __builtin_amdgcn_exp2f(fmaf(sc[u], scale2, -m));
-        sum += sc[u];
+        sc[sub][u] = __builtin_amdgcn_exp2f(fmaf(sc[sub][u], scale2, -m));
+        sum += sc[sub][u];
       }
       l += sum;
       if constexpr (DT == kBF16) {
@@ -406,7 +411,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
         for (int s = 0; s < M::kScores / 8; ++s) {
           u32x4 p;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) p[i] = bf16_pair(sc[8 * s + 2 * i], sc[8 * s + 2 * i + 1]);
+          for (int i = 0; i < 4; ++i) p[i] = bf16_pair(sc[sub][8 * s + 2 * i], sc[sub][8 * s + 2 * i + 1]);
 #pragma unroll
           for (int i = 0; i < kDT; ++i) {
             uint2 part[2];
@@ -430,7 +435,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
           for (int i = 0; i < kDT / 4; ++i) {
             const f32x4v v = *reinterpret_cast<const f32x4v*>(vl + row * RB + (((i * QW + col) ^ mix<RB>(row)) << 4));
 #pragma unroll
-            for (int k = 0; k < 4; ++k) o[4 * i + k] = M::av(v[k], sc[u], o[4 * i + k]);
+            for (int k = 0; k < 4; ++k) o[4 * i + k] = M::av(v[k], sc[sub][u], o[4 * i + k]);
           }
         }
       }

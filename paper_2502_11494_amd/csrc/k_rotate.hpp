@@ -88,6 +88,36 @@ __global__ __launch_bounds__(256) void k_norm_rotate(Rotate a, Cache c) {
   const long t = (long)blockIdx.x * (4 / W) + wave / W;
   const bool live = t < a.T;
 
+  const int L = 1 << a.lanes_shift, u = lane & (L - 1), per = kWave >> a.lanes_shift;
+  const bool used = u < a.units && live;
+  const int rot_units = a.half / VE;
+  const bool turned = u < rot_units;
+  const int rest = 2 * a.half + 2 * (u - rot_units) * VE;  // (past the turned pairs: two pieces in a row)
+  const int at0 = turned ? (a.interleaved ? 2 * u * VE : u * VE) : rest;
+  const int at1 = turned && !a.interleaved ? a.half + u * VE : at0 + VE;
+  const bool two = at1 < a.d;
+  const int heads = a.Hq + a.Hkv + (APPEND ? a.Hkv : 0);
+  // With a wave to a token two rounds of heads are asked for before the first is worked on, the first two before the
+  // angles (36 864 tokens of 28 + 4 heads 111 -> 108.5 us, 23 040 of 32 + 32 with values 207 -> 200; four at once 110 and
+  // 201, and 31 000 of 28 + 4 + 4 112 -> 128).  Four waves to a token have a few rounds each and do better the plain
+  // way (576 tokens of 64 heads, 32 bits: 10.9 us, 11.4 with the loads first).
+  constexpr int kAhead = W == 1 ? 2 : 1;
+  Piece<DT, VE> r0[kAhead] = {}, r1[kAhead] = {};
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const int head = h0 + x * W * per + (lane >> a.lanes_shift);
+      const bool is_q = head < a.Hq, is_k = !is_q && head < a.Hq + a.Hkv;
+      if (!used || head >= heads) continue;
+      const void* src = is_q ? a.q : is_k ? a.k : a.v;
+      const long row = t * (is_q ? a.q_ld : is_k ? a.k_ld : a.v_ld) +
+                       (long)(is_q ? head : is_k ? head - a.Hq : head - a.Hq - a.Hkv) * a.d;
+      r0[x] = load_piece<DT, VE>(src, row + at0);
+      if (two) r1[x] = load_piece<DT, VE>(src, row + at1);
+    }
+  };
+  if (W == 1) load(0);
+
   for (int p = lane; p < a.half; p += kWave) {
     float sn = 0.f, cs = 1.f;
     if (live) {
@@ -115,14 +145,6 @@ __global__ __launch_bounds__(256) void k_norm_rotate(Rotate a, Cache c) {
     if (!put && lane == 0 && part == 0) flag(c, bad ? kBadPage : kBadSequence);
   }
 
-  const int L = 1 << a.lanes_shift, u = lane & (L - 1), per = kWave >> a.lanes_shift;
-  const bool used = u < a.units && live;
-  const int rot_units = a.half / VE;
-  const bool turned = u < rot_units;
-  const int rest = 2 * a.half + 2 * (u - rot_units) * VE;  // (past the turned pairs: two pieces in a row)
-  const int at0 = turned ? (a.interleaved ? 2 * u * VE : u * VE) : rest;
-  const int at1 = turned && !a.interleaved ? a.half + u * VE : at0 + VE;
-  const bool two = at1 < a.d;
   float cs[VE], sn[VE];
 #pragma unroll
   for (int j = 0; j < VE; ++j) {
@@ -130,77 +152,77 @@ __global__ __launch_bounds__(256) void k_norm_rotate(Rotate a, Cache c) {
     cs[j] = v.x;
     sn[j] = v.y;
   }
-  const int heads = a.Hq + a.Hkv + (APPEND ? a.Hkv : 0);
   double l1 = 0.0;
-  for (int h0 = part * per; h0 < heads; h0 += W * per) {
-    const int head = h0 + (lane >> a.lanes_shift);
-    const bool on = used && head < heads;
-    const bool is_q = head < a.Hq, is_k = !is_q && head < a.Hq + a.Hkv;
-    const int h = is_q ? head : is_k ? head - a.Hq : head - a.Hq - a.Hkv;
-    const void* src = is_q ? a.q : is_k ? a.k : a.v;
-    const long row = t * (is_q ? a.q_ld : is_k ? a.k_ld : a.v_ld) + (long)h * a.d;
-    Piece<DT, VE> p0 = {}, p1 = {};
-    if (on) p0 = load_piece<DT, VE>(src, row + at0);
-    if (on && two) p1 = load_piece<DT, VE>(src, row + at1);
-    if (is_q || is_k) {
-      float x0[VE], x1[VE];
+  for (int h0 = part * per; h0 < heads; h0 += kAhead * W * per) {
+    if (W > 1 || h0 > 0) load(h0);
 #pragma unroll
-      for (int j = 0; j < VE; ++j) x0[j] = p0.get(j), x1[j] = p1.get(j);
-      const void* w = is_q ? a.qw : a.kw;
-      if (a.qw != nullptr || a.kw != nullptr) {
-        float ss = 0.f;
+    for (int x = 0; x < kAhead; ++x) {
+      const int head = h0 + x * W * per + (lane >> a.lanes_shift);
+      if (h0 + x * W * per >= heads) break;
+      const bool on = used && head < heads;
+      const bool is_q = head < a.Hq, is_k = !is_q && head < a.Hq + a.Hkv;
+      const int h = is_q ? head : is_k ? head - a.Hq : head - a.Hq - a.Hkv;
+      Piece<DT, VE> p0 = r0[x], p1 = r1[x];
+      if (is_q || is_k) {
+        float x0[VE], x1[VE];
 #pragma unroll
-        for (int j = 0; j < VE; ++j) ss += x0[j] * x0[j] + x1[j] * x1[j];
-        for (int o = 1; o < L; o <<= 1) ss += __shfl_xor(ss, o);
-        if (on && w != nullptr) {
-          const float r = rsqrtf(ss / (float)a.d + a.eps);
-          const Piece<DT, VE> w0 = load_piece<DT, VE>(w, at0);
-          Piece<DT, VE> w1 = {};
-          if (two) w1 = load_piece<DT, VE>(w, at1);
+        for (int j = 0; j < VE; ++j) x0[j] = p0.get(j), x1[j] = p1.get(j);
+        const void* w = is_q ? a.qw : a.kw;
+        if (a.qw != nullptr || a.kw != nullptr) {
+          float ss = 0.f;
 #pragma unroll
-          for (int j = 0; j < VE; ++j) x0[j] = x0[j] * r * w0.get(j), x1[j] = x1[j] * r * w1.get(j);
-        }
-      }
-      if (turned) {
-        if (a.interleaved) {
+          for (int j = 0; j < VE; ++j) ss += x0[j] * x0[j] + x1[j] * x1[j];
+          for (int o = 1; o < L; o <<= 1) ss += __shfl_xor(ss, o);
+          if (on && w != nullptr) {
+            const float r = rsqrtf(ss / (float)a.d + a.eps);
+            const Piece<DT, VE> w0 = load_piece<DT, VE>(w, at0);
+            Piece<DT, VE> w1 = {};
+            if (two) w1 = load_piece<DT, VE>(w, at1);
 #pragma unroll
-          for (int j = 0; j < VE / 2; ++j) {
-            const float e0 = x0[2 * j], o0 = x0[2 * j + 1], e1 = x1[2 * j], o1 = x1[2 * j + 1];
-            x0[2 * j] = e0 * cs[j] - o0 * sn[j];
-            x0[2 * j + 1] = o0 * cs[j] + e0 * sn[j];
-            x1[2 * j] = e1 * cs[VE / 2 + j] - o1 * sn[VE / 2 + j];
-            x1[2 * j + 1] = o1 * cs[VE / 2 + j] + e1 * sn[VE / 2 + j];
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < VE; ++j) {
-            const float e = x0[j], o = x1[j];
-            x0[j] = e * cs[j] - o * sn[j];
-            x1[j] = o * cs[j] + e * sn[j];
+            for (int j = 0; j < VE; ++j) x0[j] = x0[j] * r * w0.get(j), x1[j] = x1[j] * r * w1.get(j);
           }
         }
-      }
-      p0 = round_piece<DT, VE>(x0);
-      p1 = round_piece<DT, VE>(x1);
-      if (is_k && on) {  // 2*VE terms in 32 bits, their sums in 64
-        float s = 0.f;
+        if (turned) {
+          if (a.interleaved) {
 #pragma unroll
-        for (int j = 0; j < VE; ++j) s += fabsf(p0.get(j)) + (two ? fabsf(p1.get(j)) : 0.f);
-        l1 += (double)s;
+            for (int j = 0; j < VE / 2; ++j) {
+              const float e0 = x0[2 * j], o0 = x0[2 * j + 1], e1 = x1[2 * j], o1 = x1[2 * j + 1];
+              x0[2 * j] = e0 * cs[j] - o0 * sn[j];
+              x0[2 * j + 1] = o0 * cs[j] + e0 * sn[j];
+              x1[2 * j] = e1 * cs[VE / 2 + j] - o1 * sn[VE / 2 + j];
+              x1[2 * j + 1] = o1 * cs[VE / 2 + j] + e1 * sn[VE / 2 + j];
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < VE; ++j) {
+              const float e = x0[j], o = x1[j];
+              x0[j] = e * cs[j] - o * sn[j];
+              x1[j] = o * cs[j] + e * sn[j];
+            }
+          }
+        }
+        p0 = round_piece<DT, VE>(x0);
+        p1 = round_piece<DT, VE>(x1);
+        if (is_k && on) {  // 2*VE terms in 32 bits, their sums in 64
+          float s = 0.f;
+#pragma unroll
+          for (int j = 0; j < VE; ++j) s += fabsf(p0.get(j)) + (two ? fabsf(p1.get(j)) : 0.f);
+          l1 += (double)s;
+        }
       }
-    }
-    if (!on) continue;
-    if (is_q || (is_k && a.k_out != nullptr)) {
-      void* dst = is_q ? a.q_out : a.k_out;
-      const long r = t * (is_q ? a.q_out_ld : a.k_out_ld) + (long)h * a.d;
-      store_piece<DT, VE>(dst, r + at0, p0);
-      if (two) store_piece<DT, VE>(dst, r + at1, p1);
-    }
-    if (APPEND && !is_q && put) {
-      void* dst = is_k ? a.k_pool : a.v_pool;
-      const long r = slot + (long)h * c.head_ld;
-      store_piece<DT, VE>(dst, r + at0, p0);
-      if (two) store_piece<DT, VE>(dst, r + at1, p1);
+      if (!on) continue;
+      if (is_q || (is_k && a.k_out != nullptr)) {
+        void* dst = is_q ? a.q_out : a.k_out;
+        const long r = t * (is_q ? a.q_out_ld : a.k_out_ld) + (long)h * a.d;
+        store_piece<DT, VE>(dst, r + at0, p0);
+        if (two) store_piece<DT, VE>(dst, r + at1, p1);
+      }
+      if (APPEND && !is_q && put) {
+        void* dst = is_k ? a.k_pool : a.v_pool;
+        const long r = slot + (long)h * c.head_ld;
+        store_piece<DT, VE>(dst, r + at0, p0);
+        if (two) store_piece<DT, VE>(dst, r + at1, p1);
+      }
     }
   }
   if (a.l1 == nullptr) return;
