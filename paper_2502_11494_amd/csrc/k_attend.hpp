@@ -263,14 +263,17 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) pg[i] = table[min(kb + my_row + i * S::kApart, last_key) >> c.page_shift];
   };
+  // (page offsets by 32-bit products: the wider ones cost as much as a fifth of a step's exponentials)
+  auto place_of = [&](int i, int kb) {
+    int page = pg[i];
+    if ((unsigned)page >= (unsigned)c.n_pages) page = 0, bad_page = true;
+    const uint32_t row = min(kb + my_row + i * S::kApart, last_key) & row_mask;
+    return ((uint64_t)(uint32_t)page * c.page_16 + (uint64_t)row * c.row_16) << 4;
+  };
   auto load_tile = [&](int kb) {
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
-      int page = pg[i];
-      if ((unsigned)page >= (unsigned)c.n_pages) page = 0, bad_page = true;
-      const uint32_t row = min(kb + my_row + i * S::kApart, last_key) & row_mask;
-      // (32 by 32 bits: the wider products cost as much as a fifth of the step's exponentials)
-      const uint64_t off = ((uint64_t)(uint32_t)page * c.page_16 + (uint64_t)row * c.row_16) << 4;
+      const uint64_t off = place_of(i, kb);
       kr[i] = *reinterpret_cast<const u32x4*>(kp + off);
       vr[i] = *reinterpret_cast<const u32x4*>(vp + off);
     }
@@ -301,7 +304,14 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   const int lim_first = __builtin_amdgcn_readfirstlane(lim);                              // of the wave's rows
   const int lim_block = causal ? min(kv - n + token_in(a, row0), last_key) : last_key;    // of the block's
 
-  auto store_tile = [&](unsigned char* buf, int kb) {
+  auto store_keys = [&](unsigned char* to) {
+#pragma unroll
+    for (int i = 0; i < S::kLoads; ++i) {
+      const int row = my_row + i * S::kApart;
+      *reinterpret_cast<u32x4*>(to + row * RB + ((my_piece ^ mix<RB>(row)) << 4)) = my_on ? kr[i] : u32x4{0, 0, 0, 0};
+    }
+  };
+  auto store_values = [&](unsigned char* to, int kb) {
     if (kb + KT > k1) {
       // What lies behind the keys may be anything; its weight is 0, and 0 times NaN is NaN.
 #pragma unroll
@@ -319,9 +329,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
       const int row = my_row + i * S::kApart;
-      const int at = row * RB + ((my_piece ^ mix<RB>(row)) << 4);
-      *reinterpret_cast<u32x4*>(buf + at) = my_on ? kr[i] : u32x4{0, 0, 0, 0};
-      *reinterpret_cast<u32x4*>(buf + S::kTileBytes + at) = vr[i];
+      *reinterpret_cast<u32x4*>(to + row * RB + ((my_piece ^ mix<RB>(row)) << 4)) = vr[i];
     }
   };
 
@@ -344,25 +352,10 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
 #pragma unroll
   for (int i = 0; i < kDT; ++i) o[i] = acc{};
   if (threadIdx.x < WK) sh.odd_values[threadIdx.x] = 0;
-  if (steps > 0) {
-    load_tile(kfirst);
-    load_pages(kfirst + kstep);
-  }
-  __syncthreads();
 
-  for (int it = 0; it < steps; ++it) {
-    const int kb = kfirst + it * kstep;
-    unsigned char* buf = my_lds + (S::kBuffers > 1 ? (it & 1) * 2 * S::kTileBytes : 0);
-    if (S::kBuffers == 1) __builtin_amdgcn_wave_barrier();
-    store_tile(buf, kb);
-    load_tile(kb + kstep);
-    load_pages(kb + 2 * kstep);
-    if (WM > 1) __syncthreads();
-    else __builtin_amdgcn_wave_barrier();
-    const unsigned char* kl = buf;
-    const unsigned char* vl = buf + S::kTileBytes;
-    // scores of the step's keys: 32 at a time in sc[sub]
-    float sc[kSub][M::kScores];
+  // ---- the three parts of a step: scores of its keys, 32 at a time in sc[sub]; their weights; the weighted values
+  float sc[kSub][M::kScores];
+  auto scores = [&](const unsigned char* kl) {
 #pragma unroll
     for (int t = 0; t < kSub * M::kTiles; ++t) {
       const int krow = t * QW + col;
@@ -373,6 +366,8 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
 #pragma unroll
       for (int i = 0; i < M::kRegs; ++i) sc[t / M::kTiles][t % M::kTiles * M::kRegs + i] = x[i];
     }
+  };
+  auto reference = [&](int kb) {
     if (kb + KT - 1 > lim_first) {
 #pragma unroll
       for (int sub = 0; sub < kSub; ++sub)
@@ -395,49 +390,80 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
 #pragma unroll
       for (int i = 0; i < kDT; ++i) o[i] *= keep;
     }
+  };
+  auto weights = [&](int sub) {
+    float sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < M::kScores; ++u) {
+      sc[sub][u] = __builtin_amdgcn_exp2f(fmaf(sc[sub][u], scale2, -m));
+      sum += sc[sub][u];
+    }
+    l += sum;
+  };
+  // bf16: the right operand of product s of a sub-step, and the product with the values: four keys at a lane's column
+  // of 16 by the transposing read of 16 lanes
+  auto packed = [&](int sub, int s) {
+    u32x4 p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = bf16_pair(sc[sub][8 * s + 2 * i], sc[sub][8 * s + 2 * i + 1]);
+    return p;
+  };
+  auto values_bf16 = [&](const unsigned char* vl, int sub, int s, const u32x4& p) {
+    const int vrow = 4 * grp + ((lane & 15) >> 2);
+#pragma unroll
+    for (int i = 0; i < kDT; ++i) {
+      uint2 two[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int row = sub * 32 + M::kRun * (2 * s + j) + vrow;
+        const int piece = i * (QW / 8) + (QW == 32 ? 2 * ((lane >> 4) & 1) : 0) + ((lane >> 1) & 1);
+        const int at = row * RB + ((piece ^ mix<RB>(row)) << 4) + 8 * (lane & 1);
+        two[j] = __builtin_bit_cast(
+            uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(vl + at)));
+      }
+      o[i] = M::pv(u32x4{two[0].x, two[0].y, two[1].x, two[1].y}, p, o[i]);
+    }
+  };
+  // (32-bit rows: a lane's 16 bytes feed four result tiles, whose rows are therefore every fourth element of the head)
+  auto values_f32 = [&](const unsigned char* vl, int sub) {
+#pragma unroll
+    for (int u = 0; u < M::kScores; ++u) {
+      const int row = sub * 32 + M::place(u, grp);
+#pragma unroll
+      for (int i = 0; i < kDT / 4; ++i) {
+        const f32x4v v = *reinterpret_cast<const f32x4v*>(vl + row * RB + (((i * QW + col) ^ mix<RB>(row)) << 4));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[4 * i + k] = M::av(v[k], sc[sub][u], o[4 * i + k]);
+      }
+    }
+  };
+
+  if (steps > 0) {
+    load_tile(kfirst);
+    load_pages(kfirst + kstep);
+  }
+  __syncthreads();
+  for (int it = 0; it < steps; ++it) {
+    const int kb = kfirst + it * kstep;
+    unsigned char* kl = my_lds + (S::kBuffers > 1 ? (it & 1) * 2 * S::kTileBytes : 0);
+    unsigned char* vl = kl + S::kTileBytes;
+    if (S::kBuffers == 1) __builtin_amdgcn_wave_barrier();
+    store_keys(kl);
+    store_values(vl, kb);
+    load_tile(kb + kstep);
+    load_pages(kb + 2 * kstep);
+    if (WM > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
+    scores(kl);
+    reference(kb);
 #pragma unroll
     for (int sub = 0; sub < kSub; ++sub) {
-      float sum = 0.f;
-#pragma unroll
-      for (int u = 0; u < M::kScores; ++u) {
-        sc[sub][u] = __builtin_amdgcn_exp2f(fmaf(sc[sub][u], scale2, -m));
-        sum += sc[sub][u];
-      }
-      l += sum;
+      weights(sub);
       if constexpr (DT == kBF16) {
-        // values: four keys at a lane's column of 16, by the transposing read of 16 lanes
-        const int vrow = 4 * grp + ((lane & 15) >> 2);
 #pragma unroll
-        for (int s = 0; s < M::kScores / 8; ++s) {
-          u32x4 p;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) p[i] = bf16_pair(sc[sub][8 * s + 2 * i], sc[sub][8 * s + 2 * i + 1]);
-#pragma unroll
-          for (int i = 0; i < kDT; ++i) {
-            uint2 part[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const int row = sub * 32 + M::kRun * (2 * s + j) + vrow;
-              const int piece = i * (QW / 8) + (QW == 32 ? 2 * ((lane >> 4) & 1) : 0) + ((lane >> 1) & 1);
-              const int at = row * RB + ((piece ^ mix<RB>(row)) << 4) + 8 * (lane & 1);
-              part[j] = __builtin_bit_cast(
-                  uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(vl + at)));
-            }
-            o[i] = M::pv(u32x4{part[0].x, part[0].y, part[1].x, part[1].y}, p, o[i]);
-          }
-        }
+        for (int s = 0; s < M::kScores / 8; ++s) values_bf16(vl, sub, s, packed(sub, s));
       } else {
-        // (a lane's 16 bytes feed four result tiles, whose rows are therefore every fourth element of the head)
-#pragma unroll
-        for (int u = 0; u < M::kScores; ++u) {
-          const int row = sub * 32 + M::place(u, grp);
-#pragma unroll
-          for (int i = 0; i < kDT / 4; ++i) {
-            const f32x4v v = *reinterpret_cast<const f32x4v*>(vl + row * RB + (((i * QW + col) ^ mix<RB>(row)) << 4));
-#pragma unroll
-            for (int k = 0; k < 4; ++k) o[4 * i + k] = M::av(v[k], sc[sub][u], o[4 * i + k]);
-          }
-        }
+        values_f32(vl, sub);
       }
     }
   }

@@ -51,6 +51,36 @@ def test_long_prompts(dtype, n, kv):
     A.check(c, A.attend(c, scale=0.09), scale=0.09)
 
 
+@pytest.mark.parametrize("Hq,Hkv,d", [(32, 32, 128), (32, 32, 64), (36, 36, 80), (40, 8, 128)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_batches_that_fill_the_chip_with_rows(Hq, Hkv, d, causal):
+    """Batches of rows enough for the widest tiles (more than 256 of a key head for every unit twice): sequences that end
+    inside a tile, start inside one, see one key, fewer keys than they have tokens, or none."""
+    n = [1, 300, 257, 0, 64, 129, 512, 31, 255, 1, 400, 256, 200, 333, 65, 128, 300, 7, 450, 290, 256, 260, 37]
+    kv = [9, 300, 300, 5, 0, 200, 512, 31, 100, 1, 400, 700, 200, 334, 65, 191, 301, 500, 450, 290, 256, 292, 40]
+    assert sum(n) * (Hq // Hkv) // 256 * Hkv >= 512 and max(n) * (Hq // Hkv) > 128
+    c = A.make(n, kv, Hq, Hkv, d, 64, "bf16", seed=Hq)
+    A.check(c, A.attend(c, scale=d ** -0.5, causal=causal), scale=d ** -0.5, causal=causal)
+
+
+def test_odd_values_in_batches_that_fill_the_chip_with_rows():
+    n = [300, 257, 64, 129, 512, 31, 255, 400, 256, 200, 333, 65, 128, 300, 450, 290, 256, 260]
+    c = A.make(n, n, 32, 32, 64, 64, "bf16", seed=3)
+    want, want_lse, tol, lse_tol = A.reference(c, 0.125, True)
+    for b, at, value in ((1, 70, float("nan")), (4, 300, float("inf")), (4, 333, -float("inf")), (9, 0, float("nan"))):
+        c.v_pool[int(c.table[b, at // 64]), 5, at % 64] = value
+    out, lse = A.attend(c, scale=0.125)
+    ok = torch.ones((c.T, 32), dtype=torch.bool)
+    for b, at in ((1, 70), (4, 300), (9, 0)):
+        ok[int(c.cu[b]) + at:int(c.cu[b + 1]), 5] = False
+    assert bool(((out.double() - want).abs() <= tol)[ok].all())
+    assert bool(((lse.double() - want_lse).abs() <= lse_tol).all())
+    o = out.float()[:, 5]
+    first = [int(x) for x in c.cu]
+    assert torch.isnan(o[first[1] + 70:first[2]]).all() and torch.isnan(o[first[9]:first[10]]).all()
+    assert bool((o[first[4] + 300:first[4] + 333] == float("inf")).all()) and torch.isnan(o[first[4] + 333:first[5]]).all()
+
+
 @pytest.mark.parametrize("n,kv", [([1, 1, 1], [9000, 1, 4097]), ([3, 1], [5000, 12001]), ([1], [20011])])
 def test_long_contexts_of_few_rows(n, kv):
     """The work of a few rows is split along the keys and joined."""
