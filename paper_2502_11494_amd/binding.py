@@ -144,14 +144,15 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _stream(stream):
     """The hipStream_t of a torch stream, of a raw handle, or of the current stream (asked for as a
     handle: a stream object costs 3 us, as much as the launch it is for)."""
     if stream is None:
-        if _raw_stream is not None and torch.cuda.is_initialized():
-            return _raw_stream(torch.cuda.current_device())
+        if _raw_stream is not None and _raw_device is not None:
+            return _raw_stream(_raw_device())
         stream = torch.cuda.current_stream()
     return C.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
@@ -336,14 +337,14 @@ def _ints(t, what: str):
 def _rows(t, kind, T: int, heads: int, d: int, what: str):
     """(address, row stride) of a tensor of rows [T, heads*d] or [T, heads, d] with contiguous
     rows, such as a slice of a fused projection's output."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) == 2:
-        good = shape[0] == T and shape[1] == heads * d and stride[1] == 1
+    shape, stride, width = t.shape, t.stride(), heads * d
+    if shape == (T, width):
+        good = stride[1] == 1
     else:
         good = shape == (T, heads, d) and stride[2] == 1 and (heads == 1 or stride[1] == d)
     if not good or t.dtype is not kind:
-        raise ValueError(f"{what}: [{T}, {heads * d}] of {kind} with contiguous rows")
-    return t.data_ptr(), (stride[0] if T > 1 else heads * d)
+        raise ValueError(f"{what}: [{T}, {width}] of {kind} with contiguous rows")
+    return t.data_ptr(), (stride[0] if T > 1 else width)
 
 
 def _plain(t, T: int, n: int, what: str):
@@ -460,8 +461,10 @@ def dart_norm_rotate(rotation: DartRotation, q, k, pos, q_out, k_out, *, l1_out=
     l1 = _plain(l1_out, T, 1, "l1_out")
     if T == 0:
         return
-    _check(lib().dart_norm_rotate(rotation._ref, T, qp, q_ld, kp, k_ld, pp, p_ld, qo, qo_ld, ko, ko_ld, l1,
-                                  _stream(stream)), "dart_norm_rotate")
+    rc = (_lib or lib()).dart_norm_rotate(rotation._ref, T, qp, q_ld, kp, k_ld, pp, p_ld, qo, qo_ld, ko, ko_ld, l1,
+                                          _stream(stream))
+    if rc:
+        _check(rc, "dart_norm_rotate")
 
 
 def dart_norm_rotate_append(rotation: DartRotation, cache: DartCache, q, k, v, pos, q_out, k_pool, v_pool, *,
@@ -480,8 +483,10 @@ def dart_norm_rotate_append(rotation: DartRotation, cache: DartCache, q, k, v, p
     l1, st = _plain(l1_out, T, 1, "l1_out"), _status(status)
     if T == 0:
         return
-    _check(lib().dart_norm_rotate_append(rotation._ref, cache._ref, qp, q_ld, kp, k_ld, vp, v_ld, pp, p_ld, qo, qo_ld,
-                                         ko, ko_ld, l1, k_at, v_at, st, _stream(stream)), "dart_norm_rotate_append")
+    rc = (_lib or lib()).dart_norm_rotate_append(rotation._ref, cache._ref, qp, q_ld, kp, k_ld, vp, v_ld, pp, p_ld, qo,
+                                                 qo_ld, ko, ko_ld, l1, k_at, v_at, st, _stream(stream))
+    if rc:
+        _check(rc, "dart_norm_rotate_append")
 
 
 def dart_attend_workspace_bytes(cache: DartCache) -> int:
@@ -506,5 +511,7 @@ def dart_attend(cache: DartCache, q, k_pool, v_pool, out, ws, *, scale: float, c
     le, st = _plain(lse, T, Hq, "lse"), _status(status)
     if T == 0:
         return
-    _check(lib().dart_attend(cache._ref, qp, q_ld, k_at, v_at, scale, causal, o, o_ld, le, ws.data_ptr(), ws.numel(), st,
-                             _stream(stream)), "dart_attend")
+    rc = (_lib or lib()).dart_attend(cache._ref, qp, q_ld, k_at, v_at, scale, causal, o, o_ld, le, ws.data_ptr(),
+                                     ws.numel(), st, _stream(stream))
+    if rc:
+        _check(rc, "dart_attend")
