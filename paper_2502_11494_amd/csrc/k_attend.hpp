@@ -302,6 +302,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   }
   const float scale2 = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;
   const int lim_first = __builtin_amdgcn_readfirstlane(lim);                              // of the wave's rows
+  const int lim_last = row0 + wm * QW < rows ? __builtin_amdgcn_readlane(lim, 63) : -1;   // (none: no key)
   const int lim_block = causal ? min(kv - n + token_in(a, row0), last_key) : last_key;    // of the block's
 
   auto store_keys = [&](unsigned char* to) {
@@ -454,6 +455,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     load_pages(kb + 2 * kstep);
     if (WM > 1) __syncthreads();
     else __builtin_amdgcn_wave_barrier();
+    if (kb > lim_last) continue;  // (none of this wave's rows sees a key of the step)
     scores(kl);
     reference(kb);
 #pragma unroll
