@@ -61,12 +61,15 @@ __device__ __forceinline__ Seq sequence_of(const Cache& c, int b) {
   return make_sequence(c, one ? b : c.cu[b], one ? b + 1 : c.cu[b + 1], c.kv_len[b]);
 }
 
-// Keys of group g's prefix; -1 if its length or its sequences are not as they have to be.
-__device__ __forceinline__ int prefix_of(const Cache& c, int g) {
-  const int n = c.prefix_len[g], b0 = c.group_cu[g], b1 = c.group_cu[g + 1];
+// Keys of a group's prefix; -1 if its length or its sequences are not as they have to be.
+__device__ __forceinline__ int make_prefix(const Cache& c, int b0, int b1, int n) {
   if (n < 0 || n > c.max_prefix || (long)n > ((long)c.prefix_ld << c.page_shift) || b0 < 0 || b1 < b0 || b1 > c.B)
     return -1;
   return n;
+}
+
+__device__ __forceinline__ int prefix_of(const Cache& c, int g) {
+  return make_prefix(c, c.group_cu[g], c.group_cu[g + 1], c.prefix_len[g]);
 }
 
 // The offset of row `key` of a page table's keys, in elements; of page 0 if its page is none.

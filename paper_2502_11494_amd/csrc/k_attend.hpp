@@ -613,34 +613,58 @@ __global__ __launch_bounds__(256) void k_attend_join(Attend a, Cache c, int pre_
                                                      const float2* part_ml, int lanes_shift, int split_shift) {
   __shared__ f32x4v set_x[256];
   __shared__ float2 set_ml[256];
-  const long all = (long)c.T * c.Hq;
+  const int all = c.T * c.Hq;  // (2^24 at most)
   const int lane = threadIdx.x & 63, set = threadIdx.x >> lanes_shift, sub = set & ((1 << split_shift) - 1);
   const int rows_shift = 8 - lanes_shift - split_shift;  // rows of a block
-  const long first = (long)blockIdx.x << rows_shift;
-  int b = (int)(first / c.Hq);
-  if (c.cu != nullptr) b = owner_of(c.cu, c.B, b);
-  const long id = first + (set >> split_shift);
+  const int first = (int)blockIdx.x << rows_shift, id = first + (set >> split_shift);
   bool row = id < all;
-  const int t = row ? (int)(id / c.Hq) : 0, h = (int)((row ? id : 0) - (long)t * c.Hq);
-  if (c.cu == nullptr) b = t;
-  else
-    while (b + 1 < c.B && c.cu[b + 1] <= t) ++b;  // (a block's rows are a few tokens')
-  const Seq s = sequence_of(c, b);
+  const int t = row ? id / c.Hq : 0, h = row ? id - t * c.Hq : 0;
+  Seq s = {};
+  int prefix = 0;
+  if (c.B <= kWave && c.groups <= kWave) {
+    // All sequences and groups in one look: seven dependent loads less in a block's life, which is little else.
+    const int i = min(lane, c.B - 1), lo = c.cu ? c.cu[i] : i, hi = c.cu ? c.cu[i + 1] : i + 1, keys = c.kv_len[i];
+    int from = 0, to = 0, front = 0;
+    if (c.groups > 0) {
+      const int g = min(lane, c.groups - 1);
+      from = c.group_cu[g], to = c.group_cu[g + 1], front = c.prefix_len[g];
+    }
+    for (int k = 0; k < kWave >> lanes_shift; ++k) {  // the wave's rows
+      const int tk = __builtin_amdgcn_readlane(t, k << lanes_shift);
+      const unsigned long long low = __ballot(lane < c.B && lo <= tk);
+      const int b = low ? 63 - __builtin_clzll(low) : 0;
+      const Seq sk = make_sequence(c, __builtin_amdgcn_readlane(lo, b), __builtin_amdgcn_readlane(hi, b), __builtin_amdgcn_readlane(keys, b));
+      int pk = 0;
+      if (c.groups > 0) {
+        const unsigned long long before = __ballot(lane < c.groups && from <= b);
+        const int g = before ? 63 - __builtin_clzll(before) : 0;
+        const int b0 = __builtin_amdgcn_readlane(from, g), b1 = __builtin_amdgcn_readlane(to, g);
+        pk = b < b0 || b >= b1 ? -1 : make_prefix(c, b0, b1, __builtin_amdgcn_readlane(front, g));
+      }
+      if (lane >> lanes_shift == k) s = sk, prefix = pk;
+    }
+  } else {
+    int b = t;
+    if (c.cu != nullptr) {
+      b = owner_of(c.cu, c.B, first / c.Hq);
+      while (b + 1 < c.B && c.cu[b + 1] <= t) ++b;  // (a block's rows are a few tokens')
+    }
+    s = sequence_of(c, b);
+    if (c.groups > 0) {
+      int g = 0, end = c.groups;
+      while (end - g > 1) {
+        const int mid = (g + end) / 2;
+        if (c.group_cu[mid] <= b) g = mid; else end = mid;
+      }
+      prefix = b < c.group_cu[g] || b >= c.group_cu[g + 1] ? -1 : prefix_of(c, g);
+    }
+  }
   int own = s.kv;
   if (a.causal && s.kv - s.n + (t - s.tok0) + 1 < own) own = s.kv - s.n + (t - s.tok0) + 1;
   row = row && t >= s.tok0 && t < s.tok0 + s.n;  // (else no sequence's token)
-  int prefix = 0;
-  if (c.groups > 0) {
-    int g = 0, end = c.groups;
-    while (end - g > 1) {
-      const int mid = (g + end) / 2;
-      if (c.group_cu[mid] <= b) g = mid; else end = mid;
-    }
-    prefix = prefix_of(c, g);
-    if (prefix < 0 || b < c.group_cu[g] || b >= c.group_cu[g + 1]) {
-      flag(c, kBadSequence);
-      prefix = own = 0;
-    }
+  if (prefix < 0) {
+    flag(c, kBadSequence);
+    prefix = own = 0;
   }
   if (!s.valid || !row) prefix = own = 0;
   const int np = prefix > 0 ? (prefix + pre_chunk - 1) / pre_chunk : 0;
@@ -656,7 +680,7 @@ __global__ __launch_bounds__(256) void k_attend_join(Attend a, Cache c, int pre_
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j) {
       const int i = min(i0 + (j << split_shift), n - 1);  // (past the last: the last again, with no weight)
-      const long at = (i < np ? i : pre_parts + i - np) * all + id;
+      const long at = (long)(i < np ? i : pre_parts + i - np) * all + id;
       ml[j] = part_ml[at];
       y[j] = *reinterpret_cast<const f32x4v*>(part_o + at * c.d + (in ? e : 0));
     }

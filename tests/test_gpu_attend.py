@@ -280,3 +280,16 @@ def test_same_inputs_same_bits_on_any_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out.cpu().view(c.T, 8, 128), first[0]) and torch.equal(lse.cpu(), first[1])
+
+
+def test_more_sequences_and_groups_than_lanes_of_a_wave():
+    """The join then looks its rows' sequences and groups up by searches."""
+    n = [i % 3 for i in range(72)]
+    kv = [a + i * 53 % 600 for i, a in enumerate(n)]
+    c = A.make(n, kv, 4, 1, 64, 16, "bf16", seed=72)
+    A.check(c, A.attend(c, scale=0.125), scale=0.125)
+    groups = [1] * 60 + [2] * 6
+    c = A.make(n, kv, 4, 2, 64, 16, "bf16", groups=groups, prefix=[i * 37 % 300 for i in range(66)], seed=73)
+    A.check(c, A.attend(c, scale=0.125), scale=0.125)
+    c = A.make([1] * 72, [1 + x for x in kv], 4, 1, 64, 16, "f32", groups=groups, prefix=[i * 37 % 300 for i in range(66)], seed=74)
+    A.check(c, A.attend(c, scale=0.125), scale=0.125)
