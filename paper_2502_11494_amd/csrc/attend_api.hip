@@ -132,7 +132,10 @@ dart_status launch_rotate(Rotate& a, const Cache& c, hipStream_t st) {
   a.units = a.half / VE + (rest + 2 * VE - 1) / (2 * VE);
   a.lanes_shift = 0;
   while ((1 << a.lanes_shift) < a.units) ++a.lanes_shift;
-  if (a.T < 4096)
+  // Four waves share a token where there are few, or where each then has two rounds of heads or more: 36 864 tokens of
+  // 32 + 32 heads 229 us with a wave each and 213 with four, 31 000 of 28 + 4 + 4 heads 114 and 154, 32 of those 8.6 and 7.9.
+  const int rounds = ((a.Hq + a.Hkv * (APPEND ? 2 : 1)) << a.lanes_shift) / kWave;
+  if (a.T < 1024 || rounds >= 8)
     k_norm_rotate<DT, VE, 4, APPEND><<<dim3(a.T), dim3(256), 0, st>>>(a, c);
   else
     k_norm_rotate<DT, VE, 1, APPEND><<<dim3((a.T + 3) / 4), dim3(256), 0, st>>>(a, c);
@@ -187,9 +190,16 @@ long blocks_of(const Cache& c, const Parting& p) { return p.slots * c.Hkv * p.ch
 // rows: (token, head) pairs of a sequence or group at most; owners: how many of them.
 Kind plan_parting(const Cache& c, int dtype, bool prefix, long rows, int owners, int max_keys, Parting& p) {
   const int r = c.Hq / c.Hkv;
-  // 256-row tiles take the least from LDS and caches per row, where there are enough of them for the chip
-  const bool wide = dtype == DART_BF16 && c.d <= 128 && ((long)c.T * r / 256) * c.Hkv >= 512;
-  Kind kind = rows <= 32 ? kFew : wide && rows > 128 ? kWide : kMany;
+  // 256-row tiles take the least from LDS and caches per row, but each has a compute unit to itself, so that nothing
+  // hides its start and end: they pay from 1024 keys and 1.5 tiles to a unit on.  28 + 4 heads, causal, 128- and
+  // 256-row tiles: two sequences of 9216 1347 and 1258 us, one of 4096 159 and 136, one of 3600 124 and 116, one of 2048
+  // 58 and 66; 24 of 1000 291 and 283, 16 of 600 91 and 95.
+  const bool wide = dtype == DART_BF16 && c.d <= 128 && rows > 128 && max_keys >= 1024 && (long)c.T * r / 256 * c.Hkv >= 384;
+  // 16-row tiles with the keys dealt to four waves end sooner while the chip is not full (256 units of 384 keys):
+  // one sequence of 9 tokens over 300 keys, 28 + 4 heads, 11.7 us and 14.1 in 128-row tiles, over 3000 keys 13.4 and 16.2;
+  // 32 such sequences 89 and 63.  Up to 16 rows nothing is gained by reading for more.
+  const long few = std::min((long)c.T * r / 16 + owners, (long)owners * ((rows + 15) / 16)) * c.Hkv;
+  Kind kind = rows <= 16 || (rows <= 64 && few * max_keys <= 256 * 384) ? kFew : wide ? kWide : kMany;
   if (dtype == DART_F32 && c.d > 128) kind = kMany;
   const int bm = rows_of(kind, dtype, c.d);
   p = {};

@@ -33,7 +33,7 @@ __device__ __forceinline__ int token_in(const Attend& a, int row) { return (int)
 // at once where there is one.
 struct Parting {
   int prefix;      // the keys are the groups' shared prefixes (else each sequence's own)
-  int few;         // tiles of 32 rows, the keys dealt to four waves (else four waves of rows)
+  int few;         // tiles of 16 rows, the keys dealt to four waves (else four waves of rows)
   int chunk;       // keys of a part
   int chunks;
   int first_part;  // part number of the first chunk
@@ -81,11 +81,8 @@ struct Math {
     }
     return c;
   }
-  // (32-bit rows) one key of each group by one weight of each group
-  __device__ static __forceinline__ acc av(float v, float p, acc c) {
-    if constexpr (QW == 32) return __builtin_amdgcn_mfma_f32_32x32x2f32(v, p, c, 0, 0, 0);
-    else return __builtin_amdgcn_mfma_f32_16x16x4f32(v, p, c, 0, 0, 0);
-  }
+  // (32-bit rows, 16 columns) one key of each group by one weight of each group
+  __device__ static __forceinline__ acc av(float v, float p, acc c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(v, p, c, 0, 0, 0); }
   __device__ static __forceinline__ acc pv(const u32x4& v, const u32x4& p, acc c) { return qk(v, p, c); }
 };
 
@@ -188,6 +185,18 @@ struct AttendShared {
   float2 joined[5][32];
 };
 
+// out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m) with s = scale * K q, in one pass over the keys: a step takes a tile
+// of keys, S^T = K Q^T, moves the running maximum m if it has to (out and sum rescaled), and adds exp(S^T - m) and
+// V^T exp(S^T - m).  Exponentials are powers of 2; scores, maximum, sum and result are in 32 bits, the weights of bf16
+// rows are rounded to bf16 for their product.  A thread's share of the next step's keys and values is on its way in
+// registers while this one's lies in LDS; with four or eight waves of rows LDS holds two steps, so that one barrier a
+// step is enough; where the waves share out the keys each has its own tiles and there is none.
+// What bounds it: many rows, the instructions of a step that are not matrix products (two causal sequences of 9216,
+// 28 + 4 heads of 128, 1.25 ms, 0.98 PF/s of the 1.37 of a large product: the matrix cores are busy 44 % of the time, the
+// vector units 33 %, and the two overlap little; no bank conflicts; 64 queries to a wave spill, two waves half a step apart
+// or other orders of a step gain nothing); one token each, memory (32 answers over 1024 to 16 384 keys: 122 us, 4.66 TB/s
+// where a large copy moves 4.79); a few rows over a few keys, latency (131 keys: 8 us, of which 1.3 for each step of 128);
+// 32-bit rows, the matrix cores' rate (637 causal tokens of 32 heads 56 us, half of it their own time, the rest waits).
 // One block: row tile `slot` against chunk `part` of the keys of head `head`.
 template <int DT, int DP, int QW, int WM, int WK, int KT>
 __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, const Parting& sp, unsigned char* lds, AttendShared& sh,
@@ -434,7 +443,8 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
       for (int i = 0; i < kDT / 4; ++i) {
         const f32x4v v = *reinterpret_cast<const f32x4v*>(vl + row * RB + (((i * QW + col) ^ mix<RB>(row)) << 4));
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[4 * i + k] = M::av(v[k], sc[sub][u], o[4 * i + k]);
+        for (int k = 0; k < 4; ++k)
+          if constexpr (DT == kF32) o[4 * i + k] = M::av(v[k], sc[sub][u], o[4 * i + k]);
       }
     }
   };
@@ -591,7 +601,10 @@ __global__ __launch_bounds__(64 * WM * WK, DP <= 128 && (DT == kBF16 || WK == 1)
   attend_tile<DT, DP, QW, WM, WK, KT>(a, c, sp, lds, sh, slot, head, part);
 }
 
-// Prefixes and own keys in one launch: the first blocks take the prefixes, the rest fill in beside them.
+// Prefixes and own keys in one launch: the first blocks take the prefixes, the rest fill in beside them (64 answers over
+// one prefix of 9216 keys, 28 + 4 heads: 33 us with the join, of which the keys' bytes are 11 and the launch and start 10;
+// 32 prompts of 9 to 71 tokens over four prefixes of 2880, 32 heads: 128 us, 0.49 PF/s, bound by units that have two
+// tiles where others have one).
 template <int DT, int DP, int KT>
 __global__ __launch_bounds__(256, DT == kBF16 && DP <= 128 ? 2 : 1) void k_attend_both(Attend a, Cache c, Parting pre, Parting own,
                                                                                        unsigned pre_blocks) {
@@ -607,7 +620,9 @@ __global__ __launch_bounds__(256, DT == kBF16 && DP <= 128 ? 2 : 1) void k_atten
 }
 
 // Joins a row's parts.  2^lanes_shift lanes hold a row, four elements each; 2^split_shift such sets of a block
-// share one row's parts where there are many, and join through LDS.  Eight parts are asked for at once.
+// share one row's parts where there are many, and join through LDS (8 rows in 63 parts: 48 us with a set to a row, 16
+// with eight, attention included).  Eight parts are asked for at once.  Bound by latency: what a row's sequence is, its
+// parts, its result, one after the other.
 template <int DT>
 __global__ __launch_bounds__(256) void k_attend_join(Attend a, Cache c, int pre_chunk, int pre_parts, int own_chunk, const float* part_o,
                                                      const float2* part_ml, int lanes_shift, int split_shift) {

@@ -72,13 +72,14 @@ __device__ __forceinline__ Piece<DT, VE> round_piece(const float (&x)[VE]) {
   return p;
 }
 
-// Memory-bound: every row is read once and written once.  W waves share a token (W = 1 where
-// there are tokens enough).  A head lies in 2^lanes_shift lanes of two pieces of 16 bytes (8
-// where a half head of bf16 is no multiple of 8 elements): with pairs (p, p + half) piece u of the
-// first half and piece u of the second, so that both elements of a pair are in one lane and a
-// lane meets the same angles in every head.  The angles are taken once per wave, a lane per pair:
-// position * frequency in 64 bits as turns, of which the whole ones are dropped, so that a long
-// context's positions lose nothing.
+// Memory-bound: every row is read once and written once (23 040 tokens of 32 + 32 + 32 heads of 128 to their pages: 1.13 GB
+// in 211 us, 5.4 TB/s, where a large copy moves 4.8; 36 864 tokens of 28 + 4 heads 113 us, 5.3 TB/s; a single token 6.5 us,
+// the launch).  W waves share a token: one or four (launch_rotate).  A head lies in 2^lanes_shift lanes of two pieces of 16
+// bytes (8 where a half head of bf16 is no multiple of 8 elements; 9216 tokens take 28 us with pieces of 16 bytes, 33 with 8):
+// with pairs (p, p + half) piece u of the first half and piece u of the second, so that both elements of a pair are in one
+// lane and a lane meets the same angles in every head.  The angles are taken once per wave, a lane per pair:
+// position * frequency in 64 bits as turns, of which the whole ones are dropped, so that a long context's positions
+// lose nothing.  Norms are summed in 32 bits over a head's elements, the L1 norms of key rows in 64.
 template <int DT, int VE, int W, bool APPEND>
 __global__ __launch_bounds__(256) void k_norm_rotate(Rotate a, Cache c) {
   __shared__ float2 turn[4][kMaxPairs];
@@ -98,9 +99,9 @@ __global__ __launch_bounds__(256) void k_norm_rotate(Rotate a, Cache c) {
   const bool two = at1 < a.d;
   const int heads = a.Hq + a.Hkv + (APPEND ? a.Hkv : 0);
   // With a wave to a token two rounds of heads are asked for before the first is worked on, the first two before the
-  // angles (36 864 tokens of 28 + 4 heads 111 -> 108.5 us, 23 040 of 32 + 32 with values 207 -> 200; four at once 110 and
-  // 201, and 31 000 of 28 + 4 + 4 112 -> 128).  Four waves to a token have a few rounds each and do better the plain
-  // way (576 tokens of 64 heads, 32 bits: 10.9 us, 11.4 with the loads first).
+  // angles (36 864 tokens of 28 + 4 heads 111 -> 108.5 us; four at once 110, and 31 000 of 28 + 4 + 4 then take 128 instead
+  // of 112).  Four waves to a token have a few rounds each and do better the plain way (576 tokens of
+  // 64 heads, 32 bits: 10.8 us, 11.2 with two rounds, 11.5 with the loads first; 23 040 of 96 heads 211, 210 and 213).
   constexpr int kAhead = W == 1 ? 2 : 1;
   Piece<DT, VE> r0[kAhead] = {}, r1[kAhead] = {};
   auto load = [&](int h0) {

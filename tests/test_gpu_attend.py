@@ -293,3 +293,30 @@ def test_more_sequences_and_groups_than_lanes_of_a_wave():
     A.check(c, A.attend(c, scale=0.125), scale=0.125)
     c = A.make([1] * 72, [1 + x for x in kv], 4, 1, 64, 16, "f32", groups=groups, prefix=[i * 37 % 300 for i in range(66)], seed=74)
     A.check(c, A.attend(c, scale=0.125), scale=0.125)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", [(32, 32, 128), (32, 32, 64), (36, 36, 80), (40, 8, 128)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_batches_that_fill_the_chip_with_rows_and_may_have_long_contexts(Hq, Hkv, d, causal):
+    """The bound on the keys, not the keys, chooses the widest tiles: sequences as above and one of 1100 keys."""
+    n = [1, 300, 257, 0, 64, 129, 512, 31, 255, 1, 400, 256, 200, 333, 65, 128, 300, 7, 450, 290, 256, 260, 37]
+    kv = [9, 300, 300, 5, 0, 200, 512, 31, 100, 1, 400, 700, 200, 334, 65, 191, 301, 1100, 450, 290, 256, 292, 40]
+    c = A.make(n, kv, Hq, Hkv, d, 64, "bf16", seed=Hq + 1)
+    A.check(c, A.attend(c, scale=d ** -0.5, causal=causal, max_kv=5000), scale=d ** -0.5, causal=causal)
+
+
+def test_odd_values_in_the_widest_tiles():
+    n = [300, 257, 64, 129, 512, 31, 255, 400, 256, 200, 333, 65, 128, 300, 450, 290, 256, 260]
+    c = A.make(n, n, 32, 32, 64, 64, "bf16", seed=4)
+    want, want_lse, tol, lse_tol = A.reference(c, 0.125, True)
+    for b, at, value in ((1, 70, float("nan")), (4, 300, float("inf"))):
+        c.v_pool[int(c.table[b, at // 64]), 5, at % 64] = value
+    out, lse = A.attend(c, scale=0.125, max_kv=5000)
+    ok = torch.ones((c.T, 32), dtype=torch.bool)
+    for b, at in ((1, 70), (4, 300)):
+        ok[int(c.cu[b]) + at:int(c.cu[b + 1]), 5] = False
+    assert bool(((out.double() - want).abs() <= tol)[ok].all())
+    assert bool(((lse.double() - want_lse).abs() <= lse_tol).all())
+    o, first = out.float()[:, 5], [int(x) for x in c.cu]
+    assert torch.isnan(o[first[1] + 70:first[2]]).all()
+    assert bool((o[first[4] + 300:first[5]] == float("inf")).all())
