@@ -192,8 +192,8 @@ struct AttendShared {
 // registers while this one's lies in LDS; with four or eight waves of rows LDS holds two steps, so that one barrier a
 // step is enough; where the waves share out the keys each has its own tiles and there is none.
 // What bounds it: many rows, the instructions of a step that are not matrix products (two causal sequences of 9216,
-// 28 + 4 heads of 128, 1.25 ms, 0.98 PF/s of the 1.37 of a large product: the matrix cores are busy 44 % of the time, the
-// vector units 33 %, and the two overlap little; no bank conflicts; 64 queries to a wave spill, two waves half a step apart
+// 28 + 4 heads of 128, 1.26 ms, 0.97 PF/s of the 1.37 of a large product: the matrix cores are busy 44 % of the time, the
+// vector units 52 %, and the two overlap little; no bank conflicts; 64 queries to a wave spill, two waves half a step apart
 // or other orders of a step gain nothing); one token each, memory (32 answers over 1024 to 16 384 keys: 122 us, 4.66 TB/s
 // where a large copy moves 4.79); a few rows over a few keys, latency (131 keys: 8 us, of which 1.3 for each step of 128);
 // 32-bit rows, the matrix cores' rate (637 causal tokens of 32 heads 56 us, half of it their own time, the rest waits).
@@ -603,7 +603,7 @@ __global__ __launch_bounds__(64 * WM * WK, DP <= 128 && (DT == kBF16 || WK == 1)
 
 // Prefixes and own keys in one launch: the first blocks take the prefixes, the rest fill in beside them (64 answers over
 // one prefix of 9216 keys, 28 + 4 heads: 33 us with the join, of which the keys' bytes are 11 and the launch and start 10;
-// 32 prompts of 9 to 71 tokens over four prefixes of 2880, 32 heads: 128 us, 0.49 PF/s, bound by units that have two
+// 32 prompts of 9 to 71 tokens over four prefixes of 2880, 32 heads: 129 us, 0.49 PF/s, bound by units that have two
 // tiles where others have one).
 template <int DT, int DP, int KT>
 __global__ __launch_bounds__(256, DT == kBF16 && DP <= 128 ? 2 : 1) void k_attend_both(Attend a, Cache c, Parting pre, Parting own,
@@ -620,9 +620,11 @@ __global__ __launch_bounds__(256, DT == kBF16 && DP <= 128 ? 2 : 1) void k_atten
 }
 
 // Joins a row's parts.  2^lanes_shift lanes hold a row, four elements each; 2^split_shift such sets of a block
-// share one row's parts where there are many, and join through LDS (8 rows in 63 parts: 48 us with a set to a row, 16
-// with eight, attention included).  Eight parts are asked for at once.  Bound by latency: what a row's sequence is, its
-// parts, its result, one after the other.
+// share one row's parts where there are many, and join through LDS (8 rows of 16 000 keys in 63 parts: 48 us with a set to
+// a row, 16 with sixteen, attention included).  Bound by latency: what a row's sequence is, its parts, its result, one after
+// the other; with many rows by memory (42 000 rows of two parts 15 us, of which a copy would need 11 for their 55 MB).  Two
+// parts are asked for at once: eight, of which those past the last are read in vain, take 2 us more there and gain nothing
+// with 63 parts.
 template <int DT>
 __global__ __launch_bounds__(256) void k_attend_join(Attend a, Cache c, int pre_chunk, int pre_parts, int own_chunk, const float* part_o,
                                                      const float2* part_ml, int lanes_shift, int split_shift) {
@@ -688,7 +690,7 @@ __global__ __launch_bounds__(256) void k_attend_join(Attend a, Cache c, int pre_
   const bool in = e < c.d;
   float top = kLowest, l = 0.f;
   f32x4v x = {};
-  constexpr int kAtOnce = 8;
+  constexpr int kAtOnce = 2;
   for (int i0 = sub; i0 < n; i0 += kAtOnce << split_shift) {
     float2 ml[kAtOnce];
     f32x4v y[kAtOnce];

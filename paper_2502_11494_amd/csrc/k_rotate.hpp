@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256) void k_norm_rotate(Rotate a, Cache c) {
   const bool two = at1 < a.d;
   const int heads = a.Hq + a.Hkv + (APPEND ? a.Hkv : 0);
   // With a wave to a token two rounds of heads are asked for before the first is worked on, the first two before the
-  // angles (36 864 tokens of 28 + 4 heads 111 -> 108.5 us; four at once 110, and 31 000 of 28 + 4 + 4 then take 128 instead
+  // angles (36 864 tokens of 28 + 4 heads 111 -> 108.5 us; four at once 110, and 32 000 of 28 + 4 + 4 then take 128 instead
   // of 112).  Four waves to a token have a few rounds each and do better the plain way (576 tokens of
   // 64 heads, 32 bits: 10.8 us, 11.2 with two rounds, 11.5 with the loads first; 23 040 of 96 heads 211, 210 and 213).
   constexpr int kAhead = W == 1 ? 2 : 1;
