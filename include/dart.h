@@ -421,7 +421,7 @@ typedef struct dart_rotation {
  * output is unspecified.  status (DEVICE int32, or NULL) is only ever OR-ed into: the caller
  * clears it.                                                                                  */
 typedef struct dart_cache {
-  int32_t B;        /* sequences, 0..2^20                                                     */
+  int32_t B;        /* sequences, 0..2^20 (0: the call writes nothing)                        */
   int32_t Hq, Hkv;  /* query heads, key/value heads: as dart_rotation                         */
   int32_t d;        /* elements of a head: a multiple of 8, <= 256                            */
   int32_t dtype;    /* dart_dtype of q, k, v, pools and out                                   */
@@ -477,10 +477,12 @@ DART_API size_t dart_attend_workspace_bytes(const dart_cache* cache);
  * token i of sequence b sees keys j <= kv_len[b] - n_b + i with `causal`, all kv_len[b] without.  With
  * s_j = scale * <q, k_j> and m the largest of them,
  *   out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),   lse = m + ln sum_j exp(s_j - m);
- * a token that sees nothing, or only scores of -infinity, gets zeros and -infinity.  out has the layout of q; lse (optional) is
- * float[T][Hq].  Scores, sums and the running result are held in 32 bits; with bfloat16 rows the
+ * a token that sees nothing, or only scores of -infinity, gets zeros and -infinity; a token that no
+ * sequence owns is not written.  out has the layout of q; lse (optional) is float[T][Hq].  Scores, sums and the running result are held in 32 bits; with bfloat16 rows the
  * factors exp(s_j - m) are rounded to bfloat16 for the product with the values (and only there).
- * A prefix is read once for all sequences of its group.  scale is finite. */
+ * A prefix is read once for all sequences of its group.  scale is finite.
+ * T * (Hq/Hkv) is at most 2^28, and T * Hq at most 2^24 where there are prefixes or the keys of few
+ * tokens are divided over the chip (beyond: DART_ERR_SHAPE, and 0 bytes of workspace). */
 DART_API dart_status dart_attend(const dart_cache* cache, const void* q, int64_t q_ld,
                                  const void* k_pool, const void* v_pool, float scale, int32_t causal,
                                  void* out, int64_t out_ld, float* lse, void* ws, size_t ws_bytes,
