@@ -196,7 +196,8 @@ struct AttendShared {
 // vector units 52 %, and the two overlap little; no bank conflicts; 64 queries to a wave spill, two waves half a step apart
 // or other orders of a step gain nothing); one token each, memory (32 answers over 1024 to 16 384 keys: 122 us, 4.66 TB/s
 // where a large copy moves 4.79); a few rows over a few keys, latency (131 keys: 8 us, of which 1.3 for each step of 128);
-// 32-bit rows, the matrix cores' rate (637 causal tokens of 32 heads 56 us, half of it their own time, the rest waits).
+// 32-bit rows, the matrix cores' rate (637 causal tokens of 32 heads 55 us with the join's 8,
+// the matrix cores busy for 22; 4096 tokens of 28 + 4 heads 1.07 ms, 112 TFLOP/s of the 153 of a large product).
 // One block: row tile `slot` against chunk `part` of the keys of head `head`.
 template <int DT, int DP, int QW, int WM, int WK, int KT>
 __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, const Parting& sp, unsigned char* lds, AttendShared& sh,
@@ -602,7 +603,7 @@ __global__ __launch_bounds__(64 * WM * WK, DP <= 128 && (DT == kBF16 || WK == 1)
 }
 
 // Prefixes and own keys in one launch: the first blocks take the prefixes, the rest fill in beside them (64 answers over
-// one prefix of 9216 keys, 28 + 4 heads: 33 us with the join, of which the keys' bytes are 11 and the launch and start 10;
+// one prefix of 9216 keys, 28 + 4 heads: 33 us, 5 of them the join, where a copy of the keys' bytes would take 11;
 // 32 prompts of 9 to 71 tokens over four prefixes of 2880, 32 heads: 129 us, 0.49 PF/s, bound by units that have two
 // tiles where others have one).
 template <int DT, int DP, int KT>

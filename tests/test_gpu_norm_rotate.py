@@ -237,3 +237,36 @@ def test_tokens_that_have_no_place_are_flagged_and_left_out():
                                   status=status)
         torch.cuda.synchronize()
         assert int(status) == 1 and torch.equal(qo, q_good)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,d,page", [(4, 2, 64, 16), (28, 4, 128, 64), (16, 16, 128, 1), (3, 1, 40, 8)])
+def test_append_of_many_tokens(dtype, Hq, Hkv, d, page):
+    """A wave to a token, or four with several rounds of heads each: pages hold what the call without pages gives."""
+    n, kv = [700, 1, 0, 613], [1000, 1, 9, 613]
+    c = A.make(n, kv, Hq, Hkv, d, page, dtype, seed=page + d)
+    T = c.T
+    rows, pos, inv_freq, sections, qw, kw = inputs(T, Hq, Hkv, d, d, 3, dtype, True, seed=7)
+    x = rows.cuda()
+    q, k, v = x[:, :Hq * d], x[:, Hq * d:(Hq + Hkv) * d], x[:, (Hq + Hkv) * d:(Hq + 2 * Hkv) * d]
+    r = D.make_rotation(Hq, Hkv, d, A.KIND[c.dtype], inv_freq.cuda(), sections=sections, q_weight=qw.cuda(),
+                        k_weight=kw.cuda(), eps=EPS)
+    qo, q1 = (torch.empty((T, Hq * d), dtype=c.dtype, device="cuda") for _ in range(2))
+    k1 = torch.empty((T, Hkv * d), dtype=c.dtype, device="cuda")
+    kp, vp = A.pool_to_gpu(c.k_pool, "heads"), A.pool_to_gpu(c.v_pool, "heads")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    D.dart_norm_rotate(r, q, k, pos.cuda(), q1, k1)
+    D.dart_norm_rotate_append(r, A.cache_of(c, kp), q, k, v, pos.cuda(), qo, kp, vp, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0 and torch.equal(qo, q1)
+    for got, heads, w in ((q1, Hq, qw), (k1, Hkv, kw)):
+        src = q if got is q1 else k
+        want, tol = definition(src.cpu(), heads, d, d, pos, sections, inv_freq, False, w, 1.0)
+        within(got.cpu().view(T, heads, d), want, tol, c.dtype)
+    for pool, was, new in ((kp, c.k_pool, k1.cpu()), (vp, c.v_pool, v.cpu())):
+        expect = was.clone()
+        for b in range(len(n)):
+            w = torch.arange(kv[b] - n[b], kv[b])
+            expect[c.table[b].long()[w // page], :, w % page] = new[int(c.cu[b]):int(c.cu[b + 1])].reshape(-1, Hkv, d)
+        same = (pool.cpu() == expect) | (torch.isnan(pool.cpu()) & torch.isnan(expect))
+        assert bool(same.all())
