@@ -234,7 +234,11 @@ dart_status plan_attend(const Cache& c, int dtype, AttendPlan& p) {
     p.pre_kind = plan_parting(c, dtype, true, std::max(1L, (rows + c.groups - 1) / c.groups), c.groups, c.max_prefix, p.pre);
     p.parts += p.pre.chunks;
     p.own.first_part = p.pre.chunks;
-    p.both = p.own_kind != kWide && p.pre_kind != kWide && (dtype == DART_BF16 || c.d <= 128);
+    // One launch for both: 64 answers over a prefix of 9216 keys, 28 + 4 heads, 33 us and 44 in two, 32 prompts over four of 2880
+    // 126 and 143.  With 32-bit rows it takes the registers of two blocks, which costs more than a launch where there are
+    // blocks enough: 16 answers over two prefixes of 3000, 64 + 8 heads (320 blocks), 50 and 69; those 64 answers (1264) 149 and 129.
+    p.both = p.own_kind != kWide && p.pre_kind != kWide &&
+             (dtype == DART_BF16 || (c.d <= 128 && blocks_of(c, p.own) + blocks_of(c, p.pre) <= 1024));
   }
   if (blocks_of(c, p.own) + blocks_of(c, p.pre) > kMaxBlocks) return DART_ERR_SHAPE;
   if (p.parts > 1 && (long)c.T * c.Hq > kMaxJoined) return DART_ERR_SHAPE;

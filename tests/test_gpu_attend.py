@@ -320,3 +320,14 @@ def test_odd_values_in_the_widest_tiles():
     o, first = out.float()[:, 5], [int(x) for x in c.cu]
     assert torch.isnan(o[first[1] + 70:first[2]]).all()
     assert bool((o[first[4] + 300:first[5]] == float("inf")).all())
+
+
+@pytest.mark.parametrize("dtype,n,Hq,Hkv,prefix,groups", [
+    ("bf16", [500, 1, 700, 450, 0, 600, 513, 800], 28, 28, [1100, 64], [3, 5]),   # the widest tiles over the prefixes
+    ("f32", [40, 33, 1, 70] * 8, 16, 16, [300, 0, 511, 64], [9, 7, 8, 8]),          # prefixes and own keys in two launches
+])
+def test_prefixes_of_many_rows(dtype, n, Hq, Hkv, prefix, groups):
+    kv = [x + i % 5 * 13 for i, x in enumerate(n)]
+    c = A.make(n, kv, Hq, Hkv, 64, 32, dtype, groups=groups, prefix=prefix, seed=len(n))
+    for causal in (True, False):
+        A.check(c, A.attend(c, scale=0.125, causal=causal), scale=0.125, causal=causal)
