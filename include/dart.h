@@ -415,7 +415,7 @@ typedef struct dart_rotation {
  * keys, the prefix_len[g] keys of the pages prefix_pages[g*prefix_ld + ...], which are stored and
  * read once for all of them.
  * A sequence whose offsets decrease or leave 0..T, with more than max_q tokens, whose kv_len is below 0
- * or over max_kv or over pages_ld*page_size, or whose prefix is as wrong, is skipped: nothing is appended
+ * or over max_kv or over pages_n*page_size, or whose prefix is as wrong, is skipped: nothing is appended
  * for it and its output is as if it saw no key; bit 0 of *status is set.  A page number outside
  * 0..n_pages-1 where a key is needed sets bit 1: the key is not appended, or the sequence's
  * output is unspecified.  status (DEVICE int32, or NULL) is only ever OR-ed into: the caller
@@ -431,7 +431,7 @@ typedef struct dart_cache {
   const int32_t* cu_q;   /* DEVICE int32[B+1] from 0 to T, or NULL: one token each (T == B)   */
   const int32_t* kv_len; /* DEVICE int32[B]                                                   */
   const int32_t* pages;  /* DEVICE int32[B][pages_ld]                                         */
-  int32_t pages_ld;      /* entries of a row of `pages`, >= 1                                 */
+  int32_t pages_ld;      /* entries from a row of `pages` to the next, >= 1                   */
   int32_t n_pages;       /* pages of the pools, >= 1                                          */
   int32_t page_size;     /* rows of a page: a power of two, 1..2^20                           */
   int64_t page_ld, head_ld, row_ld; /* strides in elements: multiples of 8 (of 4 for 32-bit rows), d <= row_ld,
@@ -441,7 +441,10 @@ typedef struct dart_cache {
   const int32_t* group_cu;     /* DEVICE int32[groups+1] from 0 to B                          */
   const int32_t* prefix_pages; /* DEVICE int32[groups][prefix_ld]                             */
   const int32_t* prefix_len;   /* DEVICE int32[groups]                                        */
-  int32_t prefix_ld;           /* entries of a row of `prefix_pages`, >= 1                    */
+  int32_t prefix_ld;           /* entries from a row of `prefix_pages` to the next, >= 1      */
+  int32_t pages_n;             /* entries of a row of `pages`, where the table is a view of a wider one; 0: pages_ld.  No
+                                  entry past them is read                                     */
+  int32_t prefix_n;            /* the same of `prefix_pages`; 0: prefix_ld                    */
 } dart_cache;
 
 /* Norms and rotates the heads of T tokens: head h of token t of q is the d elements from t*q_ld + h*d,

@@ -67,7 +67,8 @@ class DartCache(C.Structure):
                 ("page_size", C.c_int32), ("page_ld", C.c_int64), ("head_ld", C.c_int64),
                 ("row_ld", C.c_int64), ("groups", C.c_int32), ("max_prefix", C.c_int32),
                 ("group_cu", C.c_void_p), ("prefix_pages", C.c_void_p),
-                ("prefix_len", C.c_void_p), ("prefix_ld", C.c_int32)]
+                ("prefix_len", C.c_void_p), ("prefix_ld", C.c_int32), ("pages_n", C.c_int32),
+                ("prefix_n", C.c_int32)]
 
 
 class DartError(RuntimeError):
@@ -364,6 +365,11 @@ def _status(t):
     return t.data_ptr()
 
 
+def _table(t):
+    """(row stride, entries of a row) of a page table, which may be a view of a wider one."""
+    return (t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)), t.shape[1]
+
+
 def make_rotation(Hq: int, Hkv: int, d: int, dtype: int, inv_freq: torch.Tensor, *,
                   interleaved: bool = False, sections=None,
                   q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
@@ -411,7 +417,9 @@ def make_cache(Hq: int, pool: torch.Tensor, pages: torch.Tensor, kv_len: torch.T
     c.T, c.max_q, c.max_kv = (c.B if T is None else T), max_q, max_kv
     c.cu_q = None if cu_q is None else _ints(cu_q, "cu_q").data_ptr()
     c.kv_len, c.pages = _ints(kv_len, "kv_len").data_ptr(), _ints(pages, "pages").data_ptr()
-    c.pages_ld = pages.stride(0) if c.B > 1 else pages.shape[1]
+    c.pages_ld, c.pages_n = _table(pages)
+    if c.pages_n == 0:  # (a table without columns: 0 would stand for pages_ld)
+        c.max_kv = 0
     c.n_pages, c.page_size = pool.shape[0], pool.shape[2]
     c.row_ld = pool.stride(2) if c.page_size > 1 else c.d
     c.head_ld = pool.stride(1) if c.Hkv > 1 else 0
@@ -422,8 +430,8 @@ def make_cache(Hq: int, pool: torch.Tensor, pages: torch.Tensor, kv_len: torch.T
             raise ValueError("group_cu: [groups+1], prefix_pages: [groups, n], prefix_len: [groups]")
         c.group_cu, c.prefix_len = _ints(group_cu, "group_cu").data_ptr(), _ints(prefix_len, "prefix_len").data_ptr()
         c.prefix_pages = _ints(prefix_pages, "prefix_pages").data_ptr()
-        c.prefix_ld = prefix_pages.stride(0) if c.groups > 1 else prefix_pages.shape[1]
-        c.max_prefix = max_prefix
+        c.prefix_ld, c.prefix_n = _table(prefix_pages)
+        c.max_prefix = max_prefix if c.prefix_n else 0
     c._keepalive = (pages, kv_len, cu_q, group_cu, prefix_pages, prefix_len)
     c._ref, c._heads = C.byref(c), (pool.dtype, Hq, c.Hkv, c.d, c.T)
     c._pool = (pool.shape, pool.stride())

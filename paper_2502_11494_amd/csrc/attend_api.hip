@@ -52,7 +52,7 @@ dart_status make_cache(const dart_cache* u, Cache& c) {
   if (!u) return DART_ERR_NULL;
   DART_TRY(check_heads(u->Hq, u->Hkv, u->d, u->dtype));
   if (u->B < 0 || u->B > kMaxSequences || u->T < 0 || u->T > kMaxTokens || u->max_q < 0 || u->max_kv < 0 ||
-      u->max_kv > kMaxKeys || u->pages_ld < 1 || u->n_pages < 1)
+      u->max_kv > kMaxKeys || u->pages_ld < 1 || u->pages_n < 0 || u->n_pages < 1)
     return DART_ERR_SHAPE;
   if (u->page_size < 1 || u->page_size > kMaxPage || (u->page_size & (u->page_size - 1))) return DART_ERR_SHAPE;
   if (u->row_ld < u->d || u->row_ld > kMaxPoolLd || u->head_ld < 0 || u->head_ld > kMaxPoolLd || u->page_ld < 0 ||
@@ -74,6 +74,7 @@ dart_status make_cache(const dart_cache* u, Cache& c) {
   c.kv_len = u->kv_len;
   c.pages = u->pages;
   c.pages_ld = u->pages_ld;
+  c.pages_n = u->pages_n ? u->pages_n : u->pages_ld;
   c.n_pages = u->n_pages;
   c.page_shift = __builtin_ctz((unsigned)u->page_size);
   c.page_ld = u->page_ld;
@@ -83,10 +84,11 @@ dart_status make_cache(const dart_cache* u, Cache& c) {
   c.row_16 = (uint32_t)(u->row_ld / a16);
   c.groups = u->groups;
   if (u->groups > 0) {
-    if (u->max_prefix < 0 || u->max_prefix > kMaxKeys || u->prefix_ld < 1) return DART_ERR_SHAPE;
+    if (u->max_prefix < 0 || u->max_prefix > kMaxKeys || u->prefix_ld < 1 || u->prefix_n < 0) return DART_ERR_SHAPE;
     if (!u->group_cu || !u->prefix_pages || !u->prefix_len) return DART_ERR_NULL;
     c.max_prefix = u->max_prefix;
     c.prefix_ld = u->prefix_ld;
+    c.prefix_n = u->prefix_n ? u->prefix_n : u->prefix_ld;
     c.group_cu = u->group_cu;
     c.prefix_pages = u->prefix_pages;
     c.prefix_len = u->prefix_len;

@@ -10,10 +10,10 @@ enum { kBadSequence = 1, kBadPage = 2 };  // bits of the caller's status word
 struct Cache {
   int B, Hq, Hkv, d, T, max_q, max_kv;
   const int *cu, *kv_len, *pages;
-  int pages_ld, n_pages, page_shift;
+  int pages_ld, pages_n, n_pages, page_shift;  // pages_n: entries of a row of the table
   long page_ld, head_ld, row_ld;  // elements
   uint32_t page_16, row_16;       // the same strides in units of 16 bytes
-  int groups, max_prefix, prefix_ld;
+  int groups, max_prefix, prefix_ld, prefix_n;
   const int *group_cu, *prefix_pages, *prefix_len;
   int* status;
 };
@@ -51,7 +51,7 @@ __device__ __forceinline__ Seq make_sequence(const Cache& c, int lo, int hi, int
   s.n = (hi < c.T ? hi : c.T) - s.tok0;
   if (s.n < 0) s.n = 0;
   s.kv = kv;
-  if (kv < 0 || kv > c.max_kv || (long)kv > ((long)c.pages_ld << c.page_shift)) s.valid = false;
+  if (kv < 0 || kv > c.max_kv || (long)kv > ((long)c.pages_n << c.page_shift)) s.valid = false;
   if (!s.valid) s.kv = 0;
   return s;
 }
@@ -63,7 +63,7 @@ __device__ __forceinline__ Seq sequence_of(const Cache& c, int b) {
 
 // Keys of a group's prefix; -1 if its length or its sequences are not as they have to be.
 __device__ __forceinline__ int make_prefix(const Cache& c, int b0, int b1, int n) {
-  if (n < 0 || n > c.max_prefix || (long)n > ((long)c.prefix_ld << c.page_shift) || b0 < 0 || b1 < b0 || b1 > c.B)
+  if (n < 0 || n > c.max_prefix || (long)n > ((long)c.prefix_n << c.page_shift) || b0 < 0 || b1 < b0 || b1 > c.B)
     return -1;
   return n;
 }

@@ -1,0 +1,34 @@
+"""Page tables that are views of wider ones: what the descriptor says about them."""
+import torch
+
+import paper_2502_11494_amd as D
+
+from test_attend_host import BAD_CACHE, FAKE, attend, cache  # noqa: F401
+
+
+def test_a_view_of_a_table_keeps_its_own_width():
+    pool, kv = torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16), torch.ones(4, dtype=torch.int32)
+    base = torch.zeros((4, 32), dtype=torch.int32)
+    c = D.make_cache(4, pool, base[:, 24:32], kv, 128)
+    assert (c.pages_ld, c.pages_n) == (32, 8)
+    c = D.make_cache(4, pool, base, kv, 128)
+    assert (c.pages_ld, c.pages_n) == (32, 32)
+    c = D.make_cache(4, pool, base[2:3, 5:9], kv[:1], 128)
+    assert c.pages_n == 4 and c.pages_ld >= 1
+    front = dict(group_cu=torch.tensor([0, 2, 4], dtype=torch.int32), prefix_len=torch.ones(2, dtype=torch.int32), max_prefix=99)
+    c = D.make_cache(4, pool, base[:, 24:32], kv, 128, prefix_pages=base[:2, 3:9], **front)
+    assert (c.prefix_ld, c.prefix_n, c.max_prefix) == (32, 6, 99)
+    # without columns no key has a page
+    c = D.make_cache(4, pool, base[:, 9:9], kv, 128, prefix_pages=base[:2, 3:3], **front)
+    assert c.pages_ld >= 1 and c.max_kv == 0 and c.prefix_ld >= 1 and c.max_prefix == 0
+
+
+def test_widths_of_tables_are_checked_and_default_to_the_stride():
+    groups = dict(groups=1, prefix_ld=4, max_prefix=9, group_cu=FAKE, prefix_pages=FAKE, prefix_len=FAKE)
+    need = D.dart_attend_workspace_bytes(cache(**groups))
+    assert need > 0
+    for kw in (dict(pages_n=-1), dict(prefix_n=-1)):
+        assert D.dart_attend_workspace_bytes(cache(**groups, **kw)) == 0
+        assert attend(cache(**groups, **kw)) == D.DART_ERR_SHAPE
+    assert D.dart_attend_workspace_bytes(cache(**groups, pages_n=20, prefix_n=4)) == need
+    assert D.dart_attend_workspace_bytes(cache(prefix_n=-1)) > 0  # (without groups their fields are ignored)
