@@ -174,8 +174,24 @@ __global__ __launch_bounds__(256) void k_norm_rotate(Rotate a, Cache c) {
 #pragma unroll
           for (int j = 0; j < VE; ++j) ss += x0[j] * x0[j] + x1[j] * x1[j];
           for (int o = 1; o < L; o <<= 1) ss += __shfl_xor(ss, o);
+          float v = ss / (float)a.d + a.eps;
+          // Elements over 2^60 or so have squares that 32 bits do not hold, and those under 2^-60 squares that lose their
+          // bits (which matters where eps does not outweigh them): the head and eps are then taken in other units.
+          const bool far = !(v > 0x1p-90f && v < INFINITY);
+          if (__any(far)) {
+            const float unit = !far || w == nullptr ? 1.f : v < 1.f ? 0x1p100f : 0x1p-70f;
+            ss = 0.f;
+#pragma unroll
+            for (int j = 0; j < VE; ++j) {
+              x0[j] *= unit;
+              x1[j] *= unit;
+              ss += x0[j] * x0[j] + x1[j] * x1[j];
+            }
+            for (int o = 1; o < L; o <<= 1) ss += __shfl_xor(ss, o);
+            v = ss / (float)a.d + a.eps * unit * unit;
+          }
           if (on && w != nullptr) {
-            const float r = rsqrtf(ss / (float)a.d + a.eps);
+            const float r = rsqrtf(v);
             const Piece<DT, VE> w0 = load_piece<DT, VE>(w, at0);
             Piece<DT, VE> w1 = {};
             if (two) w1 = load_piece<DT, VE>(w, at1);
