@@ -481,7 +481,8 @@ DART_API size_t dart_attend_workspace_bytes(const dart_cache* cache);
  * s_j = scale * <q, k_j> and m the largest of them,
  *   out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),   lse = m + ln sum_j exp(s_j - m);
  * a token that sees nothing, or only scores of -infinity, gets zeros and -infinity; a token that no
- * sequence owns is not written.  out has the layout of q; lse (optional) is float[T][Hq].  Scores, sums and the running result are held in 32 bits; with bfloat16 rows the
+ * sequence owns is not written.  out has the layout of q; lse (optional) is float[T][Hq].  Scores, sums and the running
+ * result are held in 32 bits (a score as s_j * log2 e: what 32 bits do not hold of that is an infinity); with bfloat16 rows the
  * factors exp(s_j - m) are rounded to bfloat16 for the product with the values (and only there).
  * A prefix is read once for all sequences of its group.  scale is finite.
  * T * (Hq/Hkv) is at most 2^28, and T * Hq at most 2^24 where there are prefixes or the keys of few

@@ -14,6 +14,10 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 // The running maximum before any score: finite, so that a hidden score's -infinity less it is -infinity
 // and no NaN, and no larger than any score.
 constexpr float kLowest = -3.402823466e38f;
+// References from here on are coarse: their spacing is 2^-9 and more.  A score's fused distance from one carries the
+// reference's own rounding, the same for all keys of a row, which the sum of weights takes out again as long as it is small: a
+// largest score of 2^32 could weigh anything from 2^-128 to 2^128.  Products rounded like the reference itself do not.
+constexpr float kCoarse = 0x1p14f;
 
 struct Attend {
   const void *q, *k_pool, *v_pool;
@@ -112,6 +116,12 @@ __device__ __forceinline__ float groups_sum(float x) {
   }
   auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Rounded by itself, not fused with a sum it is in.
+__device__ __forceinline__ float product(float x, float y) {
+#pragma clang fp contract(off)
+  return x * y;
 }
 
 // Puts 0 in the place of infinities and NaN; not 0 if there were any.  (An exponent of ones carries into
@@ -360,6 +370,10 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     return v;
   };
   float m = kLowest, l = 0.f;
+  // The weights are 2^(score * scale2 - less).  A row whose maximum is over `above` goes through the branch that moves its
+  // reference m; one whose reference is coarse does at every step, and has its scores replaced by their distances from m there.
+  float above = kLowest, less = kLowest;
+  const float back = 1.f / scale2;
 #pragma unroll
   for (int i = 0; i < kDT; ++i) o[i] = acc{};
   if (threadIdx.x < WK) sh.odd_values[threadIdx.x] = 0;
@@ -377,6 +391,18 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
 #pragma unroll
       for (int i = 0; i < M::kRegs; ++i) sc[t / M::kTiles][t % M::kTiles * M::kRegs + i] = x[i];
     }
+    if constexpr (DT == kBF16) {
+      // Three reads of keys on their way before the first product.  (Left to itself the compiler, short of registers, waits for
+      // each read right before its product: 64 answers over a prefix of 9216 35 us instead of 33.)
+      constexpr int kAll = kSub * M::kTiles * kSteps, kLead = 3;
+      __builtin_amdgcn_sched_group_barrier(0x100, kLead, 0);
+#pragma unroll
+      for (int i = 0; i < kAll - kLead; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x8, kLead, 0);
+    }
   };
   auto reference = [&](int kb) {
     if (kb + KT - 1 > lim_first) {
@@ -393,20 +419,29 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     top = groups_max<QW>(top) * scale2;
     // The reference of the exponentials follows the maximum only where it has grown by more than a factor
     // of 2^6: until then the weights are at most 64, and nothing is rescaled.
-    if (__any(top > m + 6.f)) {
+    if (__any(top > above)) {
       const float now = fmaxf(m, top);
       const float keep = __builtin_amdgcn_exp2f(m - now);
       m = now;
       l *= keep;
 #pragma unroll
       for (int i = 0; i < kDT; ++i) o[i] *= keep;
+      const bool coarse = fabsf(m) >= kCoarse && m > kLowest;
+      above = coarse ? -INFINITY : m + 6.f;
+      less = coarse ? 0.f : m;
+      if (__any(coarse)) {
+#pragma unroll
+        for (int sub = 0; sub < kSub; ++sub)
+#pragma unroll
+          for (int u = 0; u < M::kScores; ++u) sc[sub][u] = coarse ? (product(sc[sub][u], scale2) - m) * back : sc[sub][u];
+      }
     }
   };
   auto weights = [&](int sub) {
     float sum = 0.f;
 #pragma unroll
     for (int u = 0; u < M::kScores; ++u) {
-      sc[sub][u] = __builtin_amdgcn_exp2f(fmaf(sc[sub][u], scale2, -m));
+      sc[sub][u] = __builtin_amdgcn_exp2f(fmaf(sc[sub][u], scale2, -less));
       sum += sc[sub][u];
     }
     l += sum;
@@ -501,7 +536,8 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
 #pragma unroll
           for (int j = 0; j < M::kVec; ++j) w = fmaf(qf.get(j), kf.get(j), w);
         }
-        w = __builtin_amdgcn_exp2f(fmaf(groups_sum<QW>(w), scale2, -m));
+        w = groups_sum<QW>(w);
+        w = __builtin_amdgcn_exp2f(fabsf(m) >= kCoarse ? product(w, scale2) - m : fmaf(w, scale2, -m));
         if (key > lim) continue;
 #pragma unroll
         for (int x = 0; x < kQuads; ++x) {
