@@ -239,10 +239,9 @@ dart_status plan_attend(const Cache& c, int dtype, AttendPlan& p) {
     // One launch for both: 64 answers over a prefix of 9216 keys, 28 + 4 heads, 33 us and 44 in two, 32 prompts over four of 2880
     // 126 and 143.  With 32-bit rows it takes the registers of two blocks, which costs more than a launch where there are
     // blocks enough: 16 answers over two prefixes of 3000, 64 + 8 heads (320 blocks), 50 and 69; those 64 answers (1264) 149 and 129.
-    p.both = p.own_kind != kWide && p.pre_kind != kWide &&
+    p.both = p.own_kind != kWide && p.pre_kind != kWide && blocks_of(c, p.own) + blocks_of(c, p.pre) <= kMaxBlocks &&
              (dtype == DART_BF16 || (c.d <= 128 && blocks_of(c, p.own) + blocks_of(c, p.pre) <= 1024));
   }
-  if (blocks_of(c, p.own) + blocks_of(c, p.pre) > kMaxBlocks) return DART_ERR_SHAPE;
   if (p.parts > 1 && (long)c.T * c.Hq > kMaxJoined) return DART_ERR_SHAPE;
   p.own.parts = p.pre.parts = p.parts;
   auto up = [](size_t v) { return (v + kAlign - 1) / kAlign * kAlign; };
@@ -258,8 +257,16 @@ dart_status plan_attend(const Cache& c, int dtype, AttendPlan& p) {
 template <int DT, int DP, int QW, int WM, int WK, int KT>
 dart_status launch_tiles(const Attend& a, const Cache& c, const Parting& sp, hipStream_t st) {
   typedef AttendShape<DT, DP, QW, WM, WK, KT> S;
-  k_attend<DT, DP, QW, WM, WK, KT><<<dim3((unsigned)blocks_of(c, sp)), dim3(S::kThreads), S::kLds, st>>>(a, c, sp);
-  return launched();
+  // (one launch, or slices of the row tiles where it would have too many blocks: a launch takes the last `slots` of those left)
+  const long most = kMaxBlocks / ((long)c.Hkv * sp.chunks);
+  Parting left = sp;
+  while (left.slots > 0) {
+    const long slots = std::min(left.slots, most);
+    k_attend<DT, DP, QW, WM, WK, KT><<<dim3((unsigned)(slots * c.Hkv * sp.chunks)), dim3(S::kThreads), S::kLds, st>>>(a, c, left);
+    DART_TRY(launched());
+    left.slots -= slots;
+  }
+  return DART_OK;
 }
 
 template <int DP>
