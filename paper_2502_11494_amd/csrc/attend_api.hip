@@ -136,8 +136,9 @@ dart_status launch_rotate(Rotate& a, const Cache& c, hipStream_t st) {
   while ((1 << a.lanes_shift) < a.units) ++a.lanes_shift;
   // Four waves share a token where there are few, or where each then has two rounds of heads or more: 36 864 tokens of
   // 32 + 32 heads 229 us with a wave each and 213 with four, 31 000 of 28 + 4 + 4 heads 114 and 154, 32 of those 8.6 and 7.9.
+  // (2^24 blocks of 256 threads would be more than a launch takes)
   const int rounds = ((a.Hq + a.Hkv * (APPEND ? 2 : 1)) << a.lanes_shift) / kWave;
-  if (a.T < 1024 || rounds >= 8)
+  if (a.T < 1024 || (rounds >= 8 && a.T < kMaxTokens))
     k_norm_rotate<DT, VE, 4, APPEND><<<dim3(a.T), dim3(256), 0, st>>>(a, c);
   else
     k_norm_rotate<DT, VE, 1, APPEND><<<dim3((a.T + 3) / 4), dim3(256), 0, st>>>(a, c);

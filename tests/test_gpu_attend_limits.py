@@ -44,3 +44,29 @@ def test_a_token_for_each_of_the_most_sequences(packed):
         assert torch.equal(lse[x] == -float("inf"), ~some)
         off = (lse[x].double() - want).abs()[some]
         assert bool((off <= 1.01 * (e[some] + 140 * u + 8 * u * (1 + want[some].abs()))).all()), at
+
+
+def test_rotation_of_the_most_tokens():
+    """2^24 tokens of rows long enough that four waves would share one: in place, 73 GB."""
+    T, Hq, d, rot = 1 << 24, 15, 136, 8
+    width, period = (Hq + 1) * d, 1024
+    if torch.cuda.mem_get_info()[0] < 2 * T * width + (20 << 30):
+        pytest.skip("needs 93 GB of free memory")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    base = torch.randn((period, width), generator=g, device="cuda").bfloat16()
+    pos = torch.arange(period, device="cuda")
+    r = D.make_rotation(Hq, 1, d, D.DART_BF16, torch.tensor([1.0, 0.3, 0.1, 0.01], device="cuda"))
+    few = base.clone()
+    D.dart_norm_rotate(r, few[:, :Hq * d], few[:, Hq * d:], pos, few[:, :Hq * d], few[:, Hq * d:])
+    x = torch.empty((T, width), dtype=torch.bfloat16, device="cuda")
+    x.view(-1, period, width).copy_(base.expand(T // period, -1, -1))
+    l1 = torch.zeros(T, device="cuda")
+    D.dart_norm_rotate(r, x[:, :Hq * d], x[:, Hq * d:], pos.repeat(T // period), x[:, :Hq * d], x[:, Hq * d:], l1_out=l1)
+    torch.cuda.synchronize()
+    assert not torch.equal(few, base)
+    for part in x.view(-1, period, width).split(512):
+        assert bool((part == few).all())
+    assert bool((l1.view(-1, period) == l1[:period]).all())
+    assert bool(((l1[:period].double() - few[:, Hq * d:].double().abs().sum(1)).abs() <= 2.0 ** -20 * l1[:period]).all())
+    del x, part
+    torch.cuda.empty_cache()
