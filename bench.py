@@ -20,6 +20,7 @@ import argparse
 import ctypes as C
 import json
 import os
+import re
 import sys
 import time
 
@@ -40,19 +41,33 @@ TRAFFIC_FILES = {2: "hbm_traffic_multicrop_B8_N2880_D4096_bf16.txt",
                  4: "hbm_traffic_video_B4_N9216_D3584_bf16.txt"}
 
 
+def step_sources():
+    """The files that the step's kernels are built from: its translation unit and what that includes
+    (the attention calls are a unit of their own, whose files have no part in the step)."""
+    csrc = os.path.join(ROOT, "paper_2502_11494_amd", "csrc")
+    found, left = set(), [os.path.join(csrc, "dart_api.hip")]
+    while left:
+        path = left.pop()
+        if path in found:
+            continue
+        found.add(path)
+        for name in re.findall(r'^#include "([^"/]+)"', open(path).read(), re.M):
+            left.append(os.path.join(csrc, name))
+    return sorted(found)
+
+
 def measured_traffic(kernel_prefix, config=2):
     """HBM bytes per launch of a kernel from the committed rocprofv3 counter summary
     (FETCH_SIZE + WRITE_SIZE, scaled by a plain copy of known size); None if the
     kernel sources changed since the counters were taken.  An empty prefix sums all
     the kernels of one step."""
-    import glob
     import hashlib
     try:
         lines = open(os.path.join(ROOT, "profiles", TRAFFIC_FILES[config])).read().splitlines()
     except (OSError, KeyError):
         return None
     h = hashlib.sha256()
-    for path in sorted(glob.glob(os.path.join(ROOT, "paper_2502_11494_amd", "csrc", "*"))):
+    for path in step_sources():
         h.update(open(path, "rb").read())
     sha = [l.split()[1] for l in lines if l.startswith("source_sha256")]
     if not sha or sha[0] != h.hexdigest():
