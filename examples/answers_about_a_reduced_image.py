@@ -121,7 +121,7 @@ def main(images=2, N=576, width=1024, keep=64, Hq=8, Hkv=2, d=64, questions=3, p
         place = torch.arange(done - n, done, device="cuda").repeat(B) + at
         cache = D.make_cache(Hq, second.k_pool, own_table, ints([done] * B), done, T=B * n, max_q=n,
                              cu_q=ints([i * n for i in range(B + 1)]) if n > 1 else None, **shared)
-        state, _, _ = second.run(state, place.expand(3, -1).contiguous(), cache)
+        state, _, _ = second.run(state, place.expand(3, -1), cache)
         outputs.append(state)
         state = torch.tanh(state.view(B, n, width)[:, -1])  # (what a model would sample, embed and feed back)
     torch.cuda.synchronize()

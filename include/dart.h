@@ -450,7 +450,8 @@ typedef struct dart_cache {
 /* Norms and rotates the heads of T tokens: head h of token t of q is the d elements from t*q_ld + h*d,
  * of k from t*k_ld + h*d (so both may be views of a fused projection's rows); outputs likewise, and
  * q_out may be q, k_out may be k.  Bases and strides are multiples of 16 bytes.
- * pos: position ids, plane p of token t at pos[p*pos_plane_stride + t]; any value.
+ * pos: position ids, plane p of token t at pos[p*pos_plane_stride + t]; any value.  The stride is at least T, or 0: one plane
+ * stands for all.
  * l1_out (optional, float[T]): the L1 norm of every key row as it is stored (all Hkv heads, after
  * rounding): the criterion norms that dart_reduce_with_norms takes with k_out as the criterion
  * rows, good to 2^-20 of their value.                                                         */

@@ -447,7 +447,7 @@ def _pool(cache: DartCache, p, what: str):
 
 
 def _planes(pos, planes: int, T: int):
-    """(address, plane stride) of position ids [T] or [planes, T], int64."""
+    """(address, plane stride) of position ids [T] or [planes, T] (or one plane expanded to that), int64."""
     shape, stride = pos.shape, pos.stride()
     if pos.dtype is not torch.int64 or shape[-1] != T or (T > 1 and stride[-1] != 1) or (
             shape[0] != planes if len(shape) == 2 else planes != 1):

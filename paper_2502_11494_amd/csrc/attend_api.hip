@@ -156,7 +156,7 @@ dart_status set_rows(Rotate& a, int dtype, int T, const void* q, int64_t q_ld, c
                      const int64_t* pos, int64_t pos_ld, void* q_out, int64_t q_out_ld, void* k_out, int64_t k_out_ld,
                      float* l1) {
   if (!pos) return DART_ERR_NULL;
-  if (a.planes > 1 && pos_ld < T) return DART_ERR_SHAPE;
+  if (a.planes > 1 && pos_ld < T && pos_ld != 0) return DART_ERR_SHAPE;  // (0: the planes are alike)
   DART_TRY(check_rows(q, q_ld, (int64_t)a.Hq * a.d, dtype));
   DART_TRY(check_rows(k, k_ld, (int64_t)a.Hkv * a.d, dtype));
   DART_TRY(check_rows(q_out, q_out_ld, (int64_t)a.Hq * a.d, dtype));
