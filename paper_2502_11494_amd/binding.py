@@ -399,13 +399,14 @@ def make_rotation(Hq: int, Hkv: int, d: int, dtype: int, inv_freq: torch.Tensor,
 
 
 def make_cache(Hq: int, pool: torch.Tensor, pages: torch.Tensor, kv_len: torch.Tensor, max_kv: int, *,
-               T: Optional[int] = None, max_q: int = 1, cu_q: Optional[torch.Tensor] = None,
+               T: Optional[int] = None, max_q: Optional[int] = None, cu_q: Optional[torch.Tensor] = None,
                group_cu: Optional[torch.Tensor] = None, prefix_pages: Optional[torch.Tensor] = None,
                prefix_len: Optional[torch.Tensor] = None, max_prefix: int = 0) -> DartCache:
     """pool: the key pool [pages, Hkv, page_size, d], any strides with contiguous heads (so a pool
     whose memory holds [pages, page_size, Hkv, d] is passed transposed); the value pool is laid out
     like it.  pages: int32 [B, n]; kv_len: int32 [B] with the tokens of the call.  cu_q: int32 [B+1] and T
-    tokens, at most max_q of a sequence; without it one token each."""
+    tokens, at most max_q of a sequence (any number by default; a bound near the truth divides the
+    work better); without it one token each."""
     if pool.dim() != 4 or pool.stride(3) != 1 or pool.dtype not in _DTYPES:
         raise ValueError("pool: [pages, Hkv, page_size, d] with contiguous heads")
     if pages.dim() != 2 or kv_len.numel() != pages.shape[0]:
@@ -414,7 +415,8 @@ def make_cache(Hq: int, pool: torch.Tensor, pages: torch.Tensor, kv_len: torch.T
     c.B, c.Hq, c.Hkv, c.d, c.dtype = pages.shape[0], Hq, pool.shape[1], pool.shape[3], _DTYPES[pool.dtype]
     if cu_q is not None and (T is None or cu_q.numel() != c.B + 1):
         raise ValueError("cu_q: [B+1], with T")
-    c.T, c.max_q, c.max_kv = (c.B if T is None else T), max_q, max_kv
+    c.T = c.B if T is None else T
+    c.max_q, c.max_kv = (1 if cu_q is None else c.T) if max_q is None else max_q, max_kv
     c.cu_q = None if cu_q is None else _ints(cu_q, "cu_q").data_ptr()
     c.kv_len, c.pages = _ints(kv_len, "kv_len").data_ptr(), _ints(pages, "pages").data_ptr()
     c.pages_ld, c.pages_n = _table(pages)

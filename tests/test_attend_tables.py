@@ -32,3 +32,12 @@ def test_widths_of_tables_are_checked_and_default_to_the_stride():
         assert attend(cache(**groups, **kw)) == D.DART_ERR_SHAPE
     assert D.dart_attend_workspace_bytes(cache(**groups, pages_n=20, prefix_n=4)) == need
     assert D.dart_attend_workspace_bytes(cache(prefix_n=-1)) > 0  # (without groups their fields are ignored)
+
+
+def test_packed_tokens_without_a_bound_may_all_be_of_one_sequence():
+    pool, pages = torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16), torch.zeros((2, 4), dtype=torch.int32)
+    kv, cu = torch.tensor([20, 30], dtype=torch.int32), torch.tensor([0, 2, 9], dtype=torch.int32)
+    assert D.make_cache(4, pool, pages, kv, 64, T=9, cu_q=cu).max_q == 9
+    assert D.make_cache(4, pool, pages, kv, 64, T=9, max_q=7, cu_q=cu).max_q == 7
+    assert D.make_cache(4, pool, pages, kv, 64, T=9, max_q=0, cu_q=cu).max_q == 0
+    assert D.make_cache(4, pool, pages, kv, 64).max_q == 1

@@ -82,3 +82,13 @@ def test_nothing_is_appended_past_a_view():
                 if x is not None:
                     want[int(table[b, (x - 1) // page]), :, (x - 1) % page] = 1.0
             assert int(status) == bits and torch.equal(k_pool, want) and torch.equal(v_pool, want)
+
+
+def test_packed_tokens_without_a_bound_on_a_sequence():
+    c = A.make([5, 1, 0, 70], [33, 9, 4, 70], 4, 2, 64, 16, "bf16", seed=3)
+    k_pool, v_pool = c.k_pool.cuda(), c.v_pool.cuda()
+    cache = D.make_cache(4, k_pool, c.table.cuda(), torch.tensor(c.kv, dtype=torch.int32).cuda(), 70, T=c.T, cu_q=c.cu.cuda())
+    out, lse = torch.empty((c.T, 256), dtype=c.dtype, device="cuda"), torch.empty((c.T, 4), device="cuda")
+    D.dart_attend(cache, A.to_gpu(c.q), k_pool, v_pool, out, D.alloc_attend_workspace(cache), scale=0.125, lse=lse)
+    torch.cuda.synchronize()
+    A.check(c, (out.cpu().view(c.T, 4, 64), lse.cpu()), scale=0.125)
