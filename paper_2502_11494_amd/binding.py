@@ -401,12 +401,13 @@ def make_rotation(Hq: int, Hkv: int, d: int, dtype: int, inv_freq: torch.Tensor,
 def make_cache(Hq: int, pool: torch.Tensor, pages: torch.Tensor, kv_len: torch.Tensor, max_kv: int, *,
                T: Optional[int] = None, max_q: Optional[int] = None, cu_q: Optional[torch.Tensor] = None,
                group_cu: Optional[torch.Tensor] = None, prefix_pages: Optional[torch.Tensor] = None,
-               prefix_len: Optional[torch.Tensor] = None, max_prefix: int = 0) -> DartCache:
+               prefix_len: Optional[torch.Tensor] = None, max_prefix: Optional[int] = None) -> DartCache:
     """pool: the key pool [pages, Hkv, page_size, d], any strides with contiguous heads (so a pool
     whose memory holds [pages, page_size, Hkv, d] is passed transposed); the value pool is laid out
     like it.  pages: int32 [B, n]; kv_len: int32 [B] with the tokens of the call.  cu_q: int32 [B+1] and T
     tokens, at most max_q of a sequence (any number by default; a bound near the truth divides the
-    work better); without it one token each."""
+    work better); without it one token each.  max_prefix: keys of a prefix at most (by default as many as its row of
+    prefix_pages has room for)."""
     if pool.dim() != 4 or pool.stride(3) != 1 or pool.dtype not in _DTYPES:
         raise ValueError("pool: [pages, Hkv, page_size, d] with contiguous heads")
     if pages.dim() != 2 or kv_len.numel() != pages.shape[0]:
@@ -433,7 +434,8 @@ def make_cache(Hq: int, pool: torch.Tensor, pages: torch.Tensor, kv_len: torch.T
         c.group_cu, c.prefix_len = _ints(group_cu, "group_cu").data_ptr(), _ints(prefix_len, "prefix_len").data_ptr()
         c.prefix_pages = _ints(prefix_pages, "prefix_pages").data_ptr()
         c.prefix_ld, c.prefix_n = _table(prefix_pages)
-        c.max_prefix = max_prefix if c.prefix_n else 0
+        room = min(c.prefix_n * c.page_size, 1 << 27)  # (the most that is accepted)
+        c.max_prefix = room if max_prefix is None else max_prefix if c.prefix_n else 0
     c._keepalive = (pages, kv_len, cu_q, group_cu, prefix_pages, prefix_len)
     c._ref, c._heads = C.byref(c), (pool.dtype, Hq, c.Hkv, c.d, c.T)
     c._pool = (pool.shape, pool.stride())

@@ -41,3 +41,13 @@ def test_packed_tokens_without_a_bound_may_all_be_of_one_sequence():
     assert D.make_cache(4, pool, pages, kv, 64, T=9, max_q=7, cu_q=cu).max_q == 7
     assert D.make_cache(4, pool, pages, kv, 64, T=9, max_q=0, cu_q=cu).max_q == 0
     assert D.make_cache(4, pool, pages, kv, 64).max_q == 1
+
+
+def test_prefixes_without_a_bound_may_fill_their_pages():
+    pool, pages = torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16), torch.zeros((2, 4), dtype=torch.int32)
+    kv, ints = torch.tensor([20, 30], dtype=torch.int32), lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    front = dict(group_cu=ints(0, 2), prefix_pages=torch.zeros((1, 9), dtype=torch.int32), prefix_len=ints(100))
+    assert D.make_cache(4, pool, pages, kv, 64, **front).max_prefix == 9 * 16
+    assert D.make_cache(4, pool, pages, kv, 64, **front, max_prefix=100).max_prefix == 100
+    assert D.make_cache(4, pool, pages, kv, 64, **front, max_prefix=0).max_prefix == 0
+    assert D.make_cache(4, pool, pages, kv, 64).max_prefix == 0
