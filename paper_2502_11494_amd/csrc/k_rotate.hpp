@@ -125,7 +125,13 @@ __global__ __launch_bounds__(256) void k_norm_rotate(Rotate a, Cache c) {
       int plane = 0;
       for (int i = 0; i + 1 < a.planes; ++i) plane += p >= a.section_end[i];
       const double turns = (double)a.pos[plane * a.pos_ld + t] * ((double)a.inv_freq[p] * 0.15915494309189533577);
-      sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
+      // half turns in two words: what the first leaves (under 2^-25) turns the sine and cosine of it a little further
+      const double halves = 2.0 * (turns - rint(turns));
+      const float first = (float)halves, rest = (float)((halves - first) * 3.14159265358979323846);
+      float s0, c0;
+      sincospif(first, &s0, &c0);
+      sn = fmaf(c0, rest, s0);
+      cs = fmaf(-s0, rest, c0);
     }
     turn[wave][p] = make_float2(cs * a.scale, sn * a.scale);
   }
