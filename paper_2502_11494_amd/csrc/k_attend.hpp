@@ -118,6 +118,13 @@ __device__ __forceinline__ float groups_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Between the lanes' stores to their wave's tiles and its reads of them, and between those and the next stores: LDS takes a
+// wave's accesses in order, so that only the compiler has to be held to it.
+__device__ __forceinline__ void tiles_handed_over() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Rounded by itself, not fused with a sum it is in.
 __device__ __forceinline__ float product(float x, float y) {
 #pragma clang fp contract(off)
@@ -494,13 +501,13 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     const int kb = kfirst + it * kstep;
     unsigned char* kl = my_lds + (S::kBuffers > 1 ? (it & 1) * 2 * S::kTileBytes : 0);
     unsigned char* vl = kl + S::kTileBytes;
-    if (S::kBuffers == 1) __builtin_amdgcn_wave_barrier();
+    if (S::kBuffers == 1) tiles_handed_over();
     store_keys(kl);
     store_values(vl, kb);
     load_tile(kb + kstep);
     load_pages(kb + 2 * kstep);
     if (WM > 1) __syncthreads();
-    else __builtin_amdgcn_wave_barrier();
+    else tiles_handed_over();
     if (kb > lim_last) continue;  // (none of this wave's rows sees a key of the step)
     scores(kl);
     reference(kb);
