@@ -48,8 +48,8 @@ __device__ __forceinline__ Seq make_sequence(const Cache& c, int lo, int hi, int
   Seq s;
   s.valid = lo >= 0 && hi >= lo && hi <= c.T && hi - lo <= c.max_q;
   s.tok0 = lo < 0 ? 0 : lo < c.T ? lo : c.T;
-  s.n = (hi < c.T ? hi : c.T) - s.tok0;
-  if (s.n < 0) s.n = 0;
+  const int end = hi < 0 ? 0 : hi < c.T ? hi : c.T;
+  s.n = end > s.tok0 ? end - s.tok0 : 0;
   s.kv = kv;
   if (kv < 0 || kv > c.max_kv || (long)kv > ((long)c.pages_n << c.page_shift)) s.valid = false;
   if (!s.valid) s.kv = 0;
