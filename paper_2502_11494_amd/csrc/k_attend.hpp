@@ -383,7 +383,9 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   const float back = 1.f / scale2;
 #pragma unroll
   for (int i = 0; i < kDT; ++i) o[i] = acc{};
-  if (threadIdx.x < WK) sh.odd_values[threadIdx.x] = 0;
+  // (all of a wave's lanes, without a branch: kernels short of registers park some in accumulation registers about here, and the
+  // compiler puts those copies in front of the end of a short branch, where only the lanes that took it make them)
+  sh.odd_values[wk] = 0;
 
   // ---- the three parts of a step: scores of its keys, 32 at a time in sc[sub]; their weights; the weighted values
   float sc[kSub][M::kScores];
