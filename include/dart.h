@@ -412,8 +412,9 @@ typedef struct dart_rotation {
  * of its own in the cache with this call's: its last n_b = cu_q[b+1] - cu_q[b] keys belong to
  * the call's tokens, in order (dart_attend without `causal` does not ask for that).
  * Shared prefixes (groups > 0): sequences group_cu[g] .. group_cu[g+1]-1 all see, before their own
- * keys, the prefix_len[g] keys of the pages prefix_pages[g*prefix_ld + ...], which are stored and
- * read once for all of them.
+ * keys, the prefix_len[g] keys of the pages prefix_pages[g*prefix_ld + ...], which are stored
+ * once for all of them.
+ * max_kv and max_prefix bound what the device arrays may hold, and divide the work: far above the lengths they cost time.
  * A sequence whose offsets decrease or leave 0..T, with more than max_q tokens, whose kv_len is below 0
  * or over max_kv or over pages_n*page_size, or whose prefix is as wrong, is skipped: nothing is appended
  * for it and its output is as if it saw no key; bit 0 of *status is set.  A page number outside
@@ -485,7 +486,8 @@ DART_API size_t dart_attend_workspace_bytes(const dart_cache* cache);
  * sequence owns is not written.  out has the layout of q; lse (optional) is float[T][Hq].  Scores, sums and the running
  * result are held in 32 bits (a score as s_j * log2 e: what 32 bits do not hold of that is an infinity); with bfloat16 rows the
  * factors exp(s_j - m) are rounded to bfloat16 for the product with the values (and only there).
- * A prefix is read once for all sequences of its group.  scale is finite.
+ * A prefix is read once for every tile of up to 256 (token, query head) pairs of a key head, not for every sequence of its group.
+ * Heads are worked on as 64, 128 or 256 elements, whichever holds them.  scale is finite.
  * T * (Hq/Hkv) is at most 2^28, and T * Hq at most 2^24 where there are prefixes or the keys of few
  * tokens are divided over the chip (beyond: DART_ERR_SHAPE, and 0 bytes of workspace). */
 DART_API dart_status dart_attend(const dart_cache* cache, const void* q, int64_t q_ld,

@@ -190,7 +190,11 @@ struct AttendPlan {
 int rows_of(Kind k, int dtype, int d) { return k == kFew ? 16 : k == kWide ? 256 : 4 * many_columns(dtype == DART_BF16 ? kBF16 : kF32, d); }
 long blocks_of(const Cache& c, const Parting& p) { return p.slots * c.Hkv * p.chunks; }
 
-// rows: (token, head) pairs of a sequence or group at most; owners: how many of them.
+// rows: (token, head) pairs of a sequence at most, of a group on average (nothing on the host says how many sequences the
+// largest has); owners: how many of them.  Uneven groups read their prefix in smaller tiles than they could: 64 answers of 32 heads
+// over four prefixes of 2880 53 us with 16 sequences to each, 65 with 61, 1, 1 and 1.  max_keys: the caller's bound, which
+// divides the keys, whatever the lengths are: one token over 2000 keys, 28 + 4 heads, 12.4 us, 27 with a bound of 131 072; 32 of
+// them 28 and 44.
 Kind plan_parting(const Cache& c, int dtype, bool prefix, long rows, int owners, int max_keys, Parting& p) {
   const int r = c.Hq / c.Hkv;
   // 256-row tiles take the least from LDS and caches per row, but each has a compute unit to itself, so that nothing

@@ -455,7 +455,8 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     }
     l += sum;
   };
-  // bf16: the right operand of product s of a sub-step, and the product with the values: four keys at a lane's column
+  // bf16 (the matrix cores take the weights in no more bits; products for what the rounding leaves would double those with
+  // the values): the right operand of product s of a sub-step, and the product with the values: four keys at a lane's column
   // of 16 by the transposing read of 16 lanes
   auto packed = [&](int sub, int s) {
     u32x4 p;
