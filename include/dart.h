@@ -495,6 +495,96 @@ DART_API dart_status dart_attend(const dart_cache* cache, const void* q, int64_t
                                  void* out, int64_t out_ld, float* lse, void* ws, size_t ws_bytes,
                                  int32_t* status, void* stream);
 
+/* ---- a cache held in 4 bits -----------------------------------------------------------------
+ * The same cache with a quarter of the bytes.  A head's row is cut into blocks of 32 values (the last one filled up
+ * with zeros); a block is 32 codes of 4 bits and one byte e, its scale 2^(e - 127).  A code is a sign (bit 3) and one of
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 (bits 0-2: 0..7); the value is their product, which bfloat16 and 32 bits hold exactly.
+ * e is the smallest from 0 to 252 that leaves the block's largest value under 7 * 2^(e - 127) (252: whatever it is), and a
+ * value becomes the nearest of the 15, a tie the even code, the largest where it lies beyond.  A block with an infinity or
+ * NaN has e = 255 and is read as NaN throughout.
+ * A pool is two arrays: `codes` (16-byte aligned) and `scales`.  With W = d rounded up to 32, the strides page_ld, head_ld and
+ * row_ld of its dart_cache count values and are multiples of 32, W <= row_ld: key head h of row r of page p has value i at bit
+ * 4 * (x + i) of codes, x = p*page_ld + h*head_ld + r*row_ld (the even value of a byte in its low half), and the
+ * scale of block j at scales[x / 32 + j].  dtype is that of the rows (k, v, q, out).  Everything else of dart_cache holds as
+ * it stands there.                                                                            */
+
+/* Writes key and value rows (laid out as in dart_norm_rotate_append, keys turned already) to their places in 4-bit pages:
+ * token i of sequence b becomes key kv_len[b] - n_b + i, so kv_len[b] >= n_b is required. */
+DART_API dart_status dart_append_4bit(const dart_cache* cache, const void* k, int64_t k_ld, const void* v, int64_t v_ld,
+                                      void* k_codes, void* k_scales, void* v_codes, void* v_scales, int32_t* status,
+                                      void* stream);
+
+/* The other way: the rows of the call's tokens as the pages hold them (all keys of sequence b with n_b = kv_len[b]), e.g. as
+ * the criterion rows of dart_reduce.  k_out or v_out may be NULL; their pools are then not looked at.  Rows of tokens that have
+ * no key are left as they were. */
+DART_API dart_status dart_read_4bit(const dart_cache* cache, const void* k_codes, const void* k_scales, const void* v_codes,
+                                    const void* v_scales, void* k_out, int64_t k_ld, void* v_out, int64_t v_ld,
+                                    int32_t* status, void* stream);
+
+/* Bytes of workspace dart_attend_4bit needs for this descriptor (host arithmetic only; 0 if it is invalid). */
+DART_API size_t dart_attend_4bit_workspace_bytes(const dart_cache* cache);
+
+/* dart_attend with the keys and values that the codes stand for; numerics and limits are its own. */
+DART_API dart_status dart_attend_4bit(const dart_cache* cache, const void* q, int64_t q_ld, const void* k_codes,
+                                      const void* k_scales, const void* v_codes, const void* v_scales, float scale,
+                                      int32_t causal, void* out, int64_t out_ld, float* lse, void* ws, size_t ws_bytes,
+                                      int32_t* status, void* stream);
+
+/* ---- eviction -------------------------------------------------------------------------------
+ * A cache that grows with its answers is cut to the keys that attention uses: the weight of every key is gathered while the
+ * answers are made, and from time to time the keys that gathered least are dropped, each key head choosing its own.
+ * Weights are float[n_pages][Hkv][page_size], contiguous: that of key head h of row r of page p at
+ * (p*Hkv + h)*page_size + r, so that the page table of the keys is theirs too.  Both calls take pools of rows
+ * (k_scales and v_scales NULL) or held in 4 bits (codes and scales); `four_bit` says so where no pool is given.          */
+
+/* Bytes of workspace dart_attend_weights needs for this descriptor (host arithmetic only; 0 if it is invalid). */
+DART_API size_t dart_attend_weights_workspace_bytes(const dart_cache* cache, int32_t four_bit);
+
+/* What the keys gather from the call's tokens.  For key j of a sequence (or of a group's prefix), per key head,
+ *   w_j <- carry * w_j + sum exp(scale * <q, k_j> - lse)
+ * over the (token, query head of the key head) pairs that see it, as dart_attend defines that; q, lse and causal as they went
+ * to it or came from it.  Keys that belong to the call's tokens start from 0, whatever their weight was, and with carry 0
+ * all do (what was there is not read).  A pair whose lse is -infinity gives nothing; another one that is no number, or
+ * infinite, goes into the weights of the keys it sees.  The weights of a sequence (or group) without tokens, and of one that is
+ * skipped, are left as they were; a group with a sequence that is skipped is skipped.  Sums in 32 bits, in a fixed order; a
+ * factor is as good as lse is, 2^-24 of its magnitude.  scale and carry are finite.  T * (Hq/Hkv) is at most 2^28, and
+ * B * Hkv times max_kv in tiles of 128 keys at most 2^30 (beyond: DART_ERR_SHAPE, and 0 bytes of workspace). */
+DART_API dart_status dart_attend_weights(const dart_cache* cache, const void* q, int64_t q_ld, const void* k_pool,
+                                         const void* k_scales, const float* lse, float scale, int32_t causal, float carry,
+                                         float* weights, void* ws, size_t ws_bytes, int32_t* status, void* stream);
+
+/* How many keys a sequence keeps (host memory, plain data): of kv keys
+ *   min(kv, max(K, first + recent)),   K = budget, or floor(kv * ratio_num / ratio_den) where budget is 0. */
+typedef struct dart_eviction {
+  int32_t budget;    /* 0..: keys, or 0: the ratio counts                                     */
+  int32_t ratio_num; /* 0..ratio_den                                                          */
+  int32_t ratio_den; /* >= 1 where it counts                                                  */
+  int32_t first;     /* keys at the front that are always kept, 0..2^27                       */
+  int32_t recent;    /* keys at the end that are always kept, 0..2^27                         */
+} dart_eviction;
+
+/* The most keys that a sequence of max_kv keeps: the entries that a row of `kept` needs (-1: invalid). */
+DART_API int32_t dart_evict_most(const dart_cache* cache, const dart_eviction* eviction, int32_t four_bit);
+
+/* Bytes of workspace dart_evict needs (host arithmetic only; 0 if a descriptor is invalid). */
+DART_API size_t dart_evict_workspace_bytes(const dart_cache* cache, const dart_eviction* eviction, int32_t four_bit);
+
+/* Cuts every sequence of the cache: each key head keeps the first and the recent keys, and of those between the ones of largest
+ * weight, of equals the first; NaN counts as less than any weight.  Kept keys keep their order and move, in place, to the
+ * front of the sequence's pages, values with them.  What lies behind them is unspecified, the pages there are free.
+ *   weights_out  optional, laid out like weights and may be weights: the kept keys' weights, moved like them
+ *   kept         optional, int32 [B][Hkv] rows kept_ld apart: the places that the kept keys had, ascending
+ *   kv_len_out   int32 [B]: keys of each sequence after the call; may be the array that cache->kv_len names
+ * The tokens of the descriptor (T, cu_q, max_q) and its groups play no part; to cut prefixes describe them as sequences.  A
+ * sequence whose kv_len is below 0 or over max_kv or its pages is skipped and bit 0 of *status set.  Keys in pages outside 0..n_pages-1
+ * count as less than any weight and are not moved, and bit 1 is set.  Pages that are named twice for keys of this call, by one
+ * sequence or by two, hold unspecified rows afterwards unless all of them keep all keys.  B * Hkv times the
+ * keys kept is at most 2^40. */
+DART_API dart_status dart_evict(const dart_cache* cache, const dart_eviction* eviction, void* k_pool, void* k_scales,
+                                void* v_pool, void* v_scales, const float* weights, float* weights_out, int32_t* kept,
+                                int64_t kept_ld, int32_t* kv_len_out, void* ws, size_t ws_bytes, int32_t* status,
+                                void* stream);
+
 /* Static, NUL-terminated description of a status code. */
 DART_API const char* dart_strerror(dart_status status);
 

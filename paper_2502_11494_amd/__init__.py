@@ -5,8 +5,12 @@ from .binding import (DART_BF16, DART_ERR_ALIGN, DART_ERR_BUDGET, DART_ERR_DEVIC
                       DART_ERR_STATIC_LIMIT,
                       DART_ERR_WORKSPACE, DART_F32, DART_OK, DART_PIVOT_MAX_L1,
                       DART_PIVOT_GIVEN, DART_PIVOT_MIN_L1, DART_PIVOT_RANDOM, DART_SCORE_MAX, DART_SCORE_MIN,
-                      DART_SCORE_PER_PIVOT, DartCache, DartDesc, DartError, DartRotation, DartRowTensor,
-                      alloc_attend_workspace, alloc_workspace, dart_attend, dart_attend_workspace_bytes,
+                      DART_SCORE_PER_PIVOT, DartCache, DartDesc, DartError, DartEviction, DartRotation, DartRowTensor,
+                      alloc_attend_4bit_workspace, alloc_attend_weights_workspace, alloc_attend_workspace,
+                      alloc_evict_workspace, alloc_pool_4bit, alloc_workspace, dart_append_4bit, dart_attend,
+                      dart_attend_4bit, dart_attend_4bit_workspace_bytes, dart_attend_weights,
+                      dart_attend_weights_workspace_bytes, dart_evict, dart_evict_most, dart_evict_workspace_bytes,
+                      dart_read_4bit, make_cache_4bit, make_eviction, dart_attend_workspace_bytes,
                       dart_compact_sequences,
                       dart_device_status, dart_duplication_scores, dart_gather_compact,
                       dart_device_status_static, dart_probe_mfma_dot32, dart_reduce,

@@ -30,6 +30,9 @@ EXPORTS = ("dart_workspace_bytes", "dart_select_pivots", "dart_duplication_score
            "dart_score_tile_shape_first_read", "dart_reduce_with_norms",
            "dart_device_status", "dart_score_tolerance", "dart_norm_rotate",
            "dart_norm_rotate_append", "dart_attend_workspace_bytes", "dart_attend",
+           "dart_append_4bit", "dart_read_4bit", "dart_attend_4bit_workspace_bytes", "dart_attend_4bit",
+           "dart_attend_weights_workspace_bytes", "dart_attend_weights", "dart_evict_most",
+           "dart_evict_workspace_bytes", "dart_evict",
            "dart_strerror")
 
 
@@ -69,6 +72,12 @@ class DartCache(C.Structure):
                 ("group_cu", C.c_void_p), ("prefix_pages", C.c_void_p),
                 ("prefix_len", C.c_void_p), ("prefix_ld", C.c_int32), ("pages_n", C.c_int32),
                 ("prefix_n", C.c_int32)]
+
+
+class DartEviction(C.Structure):
+    """Mirror of `struct dart_eviction`."""
+    _fields_ = [("budget", C.c_int32), ("ratio_num", C.c_int32), ("ratio_den", C.c_int32),
+                ("first", C.c_int32), ("recent", C.c_int32)]
 
 
 class DartError(RuntimeError):
@@ -116,13 +125,27 @@ def lib():
         L.dart_attend_workspace_bytes.argtypes = [cp]
         L.dart_attend_workspace_bytes.restype = sz
         L.dart_attend.argtypes = [cp, vp, i64, vp, vp, f32, i32, vp, i64, vp, vp, sz, vp, vp]
+        L.dart_append_4bit.argtypes = [cp, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp]
+        L.dart_read_4bit.argtypes = [cp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp]
+        L.dart_attend_4bit_workspace_bytes.argtypes = [cp]
+        L.dart_attend_4bit_workspace_bytes.restype = sz
+        L.dart_attend_4bit.argtypes = [cp, vp, i64, vp, vp, vp, vp, f32, i32, vp, i64, vp, vp, sz, vp, vp]
+        ep = C.POINTER(DartEviction)
+        L.dart_attend_weights_workspace_bytes.argtypes = [cp, i32]
+        L.dart_attend_weights_workspace_bytes.restype = sz
+        L.dart_attend_weights.argtypes = [cp, vp, i64, vp, vp, vp, f32, i32, f32, vp, vp, sz, vp, vp]
+        L.dart_evict_most.argtypes = [cp, ep, i32]
+        L.dart_evict_workspace_bytes.argtypes = [cp, ep, i32]
+        L.dart_evict_workspace_bytes.restype = sz
+        L.dart_evict.argtypes = [cp, ep, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, sz, vp, vp]
         for name in ("dart_select_pivots", "dart_duplication_scores", "dart_topk_keep",
                      "dart_gather_compact", "dart_compact_sequences", "dart_reduce",
                      "dart_reduce_profiled", "dart_device_status", "dart_reduce_static",
                      "dart_device_status_static", "dart_probe_mfma_dot32",
                      "dart_score_tile_shape", "dart_score_tile_shape_first_read",
                      "dart_reduce_with_norms", "dart_norm_rotate", "dart_norm_rotate_append",
-                     "dart_attend"):
+                     "dart_attend", "dart_append_4bit", "dart_read_4bit", "dart_attend_4bit",
+                     "dart_attend_weights", "dart_evict"):
             getattr(L, name).restype = C.c_int
         L.dart_score_tolerance.argtypes = [i32]
         L.dart_score_tolerance.restype = C.c_double
@@ -410,10 +433,16 @@ def make_cache(Hq: int, pool: torch.Tensor, pages: torch.Tensor, kv_len: torch.T
     prefix_pages has room for)."""
     if pool.dim() != 4 or pool.stride(3) != 1 or pool.dtype not in _DTYPES:
         raise ValueError("pool: [pages, Hkv, page_size, d] with contiguous heads")
+    return _cache(Hq, pool.shape[3], pool.dtype, pool, 1, pages, kv_len, max_kv, T, max_q, cu_q, group_cu, prefix_pages, prefix_len,
+                  max_prefix)
+
+
+def _cache(Hq, d, kind, pool, values, pages, kv_len, max_kv, T, max_q, cu_q, group_cu, prefix_pages, prefix_len, max_prefix):
+    """The descriptor; values: of an element of the pool."""
     if pages.dim() != 2 or kv_len.numel() != pages.shape[0]:
         raise ValueError("pages: [B, n], kv_len: [B]")
     c = DartCache()
-    c.B, c.Hq, c.Hkv, c.d, c.dtype = pages.shape[0], Hq, pool.shape[1], pool.shape[3], _DTYPES[pool.dtype]
+    c.B, c.Hq, c.Hkv, c.d, c.dtype = pages.shape[0], Hq, pool.shape[1], d, _DTYPES[kind]
     if cu_q is not None and (T is None or cu_q.numel() != c.B + 1):
         raise ValueError("cu_q: [B+1], with T")
     c.T = c.B if T is None else T
@@ -424,9 +453,9 @@ def make_cache(Hq: int, pool: torch.Tensor, pages: torch.Tensor, kv_len: torch.T
     if c.pages_n == 0:  # (a table without columns: 0 would stand for pages_ld)
         c.max_kv = 0
     c.n_pages, c.page_size = pool.shape[0], pool.shape[2]
-    c.row_ld = pool.stride(2) if c.page_size > 1 else c.d
-    c.head_ld = pool.stride(1) if c.Hkv > 1 else 0
-    c.page_ld = pool.stride(0) if c.n_pages > 1 else 0
+    c.row_ld = pool.stride(2) * values if c.page_size > 1 else pool.shape[3] * values
+    c.head_ld = pool.stride(1) * values if c.Hkv > 1 else 0
+    c.page_ld = pool.stride(0) * values if c.n_pages > 1 else 0
     if group_cu is not None:
         c.groups = prefix_len.numel()
         if group_cu.numel() != c.groups + 1 or prefix_pages.dim() != 2 or prefix_pages.shape[0] != c.groups:
@@ -437,14 +466,14 @@ def make_cache(Hq: int, pool: torch.Tensor, pages: torch.Tensor, kv_len: torch.T
         room = min(c.prefix_n * c.page_size, 1 << 27)  # (the most that is accepted)
         c.max_prefix = room if max_prefix is None else max_prefix if c.prefix_n else 0
     c._keepalive = (pages, kv_len, cu_q, group_cu, prefix_pages, prefix_len)
-    c._ref, c._heads = C.byref(c), (pool.dtype, Hq, c.Hkv, c.d, c.T)
-    c._pool = (pool.shape, pool.stride())
+    c._ref, c._heads = C.byref(c), (kind, Hq, c.Hkv, c.d, c.T)
+    c._pool, c._kind, c._scales = (pool.shape, pool.stride()), pool.dtype, None
     return c
 
 
 def _pool(cache: DartCache, p, what: str):
     shape, stride = cache._pool
-    if p.shape != shape or p.dtype is not cache._heads[0] or (
+    if p.shape != shape or p.dtype is not cache._kind or (
             p.stride() != stride and any(a != b for a, b, n in zip(p.stride(), stride, shape) if n > 1)):
         raise ValueError(f"{what}: shape, strides and dtype of the pool the descriptor was made for")
     return p.data_ptr()
@@ -527,3 +556,199 @@ def dart_attend(cache: DartCache, q, k_pool, v_pool, out, ws, *, scale: float, c
                                      ws.numel(), st, _stream(stream))
     if rc:
         _check(rc, "dart_attend")
+
+
+# ---- a cache held in 4 bits ------------------------------------------------------------------
+
+
+def alloc_pool_4bit(n_pages: int, Hkv: int, page_size: int, d: int, device="cuda"):
+    """A pool held in 4 bits, all zeros: (codes, scales), uint8 [n_pages, Hkv, page_size, 16 or 1 times the blocks of
+    32 values in a head]."""
+    blocks = -(-d // 32)
+    return tuple(torch.zeros((n_pages, Hkv, page_size, blocks * n), dtype=torch.uint8, device=device) for n in (16, 1))
+
+
+def make_cache_4bit(Hq: int, d: int, dtype: int, pool, pages: torch.Tensor, kv_len: torch.Tensor, max_kv: int, *,
+                    T: Optional[int] = None, max_q: Optional[int] = None, cu_q: Optional[torch.Tensor] = None,
+                    group_cu: Optional[torch.Tensor] = None, prefix_pages: Optional[torch.Tensor] = None,
+                    prefix_len: Optional[torch.Tensor] = None, max_prefix: Optional[int] = None) -> DartCache:
+    """make_cache for pools held in 4 bits.  pool: (codes, scales) as alloc_pool_4bit makes them, any strides with contiguous
+    heads that are alike for both (a pool whose memory holds [pages, page_size, Hkv, ...] is passed transposed);
+    d, dtype: elements of a head and dtype of the rows."""
+    codes, scales = pool
+    blocks = -(-d // 32)
+    if codes.dim() != 4 or codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or dtype not in _KINDS or (
+            codes.shape != (*scales.shape[:3], 16 * blocks)) or scales.shape[3] != blocks or codes.stride(3) != 1 or (
+            blocks > 1 and scales.stride(3) != 1) or any(
+            n > 1 and x != 16 * y for n, x, y in zip(codes.shape[:3], codes.stride(), scales.stride())):
+        raise ValueError(f"pool: uint8 codes [pages, Hkv, page_size, {16 * blocks}] and scales [..., {blocks}], heads contiguous, "
+                         "strides alike")
+    c = _cache(Hq, d, _KINDS[dtype], codes, 2, pages, kv_len, max_kv, T, max_q, cu_q, group_cu, prefix_pages, prefix_len, max_prefix)
+    c._scales = (scales.shape, scales.stride())
+    return c
+
+
+def _held(cache: DartCache, p, what: str):
+    """Addresses of (codes, scales), or of a pool of rows and None."""
+    if cache._scales is None:
+        return _pool(cache, p, what), None
+    if not isinstance(p, (tuple, list)) or len(p) != 2:
+        raise ValueError(f"{what}: (codes, scales)")
+    codes, scales = p
+    shape, stride = cache._scales
+    if scales.shape != shape or scales.dtype is not torch.uint8 or (
+            scales.stride() != stride and any(a != b for a, b, n in zip(scales.stride(), stride, shape) if n > 1)):
+        raise ValueError(f"{what}: scales as of the pool the descriptor was made for")
+    return _pool(cache, codes, what), scales.data_ptr()
+
+
+def _codes(cache: DartCache, p, what: str):
+    if cache._scales is None:
+        raise ValueError("cache: of make_cache_4bit")
+    return _held(cache, p, what)
+
+
+def _workspace(n: int, where: str, device):
+    if n == 0:
+        raise DartError(DART_ERR_SHAPE, where)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def dart_append_4bit(cache: DartCache, k, v, k_pool, v_pool, *, status=None, stream=None):
+    """Key and value rows [T, Hkv*d] of the cache's tokens to their places in pages held in 4 bits."""
+    kind, _, Hkv, d, T = cache._heads
+    kp, k_ld = _rows(k, kind, T, Hkv, d, "k")
+    vp, v_ld = _rows(v, kind, T, Hkv, d, "v")
+    kc, ks = _codes(cache, k_pool, "k_pool")
+    vc, vs = _codes(cache, v_pool, "v_pool")
+    st = _status(status)
+    if T == 0:
+        return
+    rc = (_lib or lib()).dart_append_4bit(cache._ref, kp, k_ld, vp, v_ld, kc, ks, vc, vs, st, _stream(stream))
+    if rc:
+        _check(rc, "dart_append_4bit")
+
+
+def dart_read_4bit(cache: DartCache, k_pool, v_pool, k_out=None, v_out=None, *, status=None, stream=None):
+    """The rows [T, Hkv*d] of the cache's tokens as the pages hold them into k_out and v_out (either may be None)."""
+    kind, _, Hkv, d, T = cache._heads
+    ko, k_ld = (None, 0) if k_out is None else _rows(k_out, kind, T, Hkv, d, "k_out")
+    vo, v_ld = (None, 0) if v_out is None else _rows(v_out, kind, T, Hkv, d, "v_out")
+    kc, ks = (None, None) if k_out is None else _codes(cache, k_pool, "k_pool")
+    vc, vs = (None, None) if v_out is None else _codes(cache, v_pool, "v_pool")
+    st = _status(status)
+    if T == 0:
+        return
+    rc = (_lib or lib()).dart_read_4bit(cache._ref, kc, ks, vc, vs, ko, k_ld, vo, v_ld, st, _stream(stream))
+    if rc:
+        _check(rc, "dart_read_4bit")
+
+
+def dart_attend_4bit_workspace_bytes(cache: DartCache) -> int:
+    return int(lib().dart_attend_4bit_workspace_bytes(C.byref(cache)))
+
+
+def alloc_attend_4bit_workspace(cache: DartCache, device="cuda") -> torch.Tensor:
+    return _workspace(dart_attend_4bit_workspace_bytes(cache), "dart_attend_4bit_workspace_bytes", device)
+
+
+def dart_attend_4bit(cache: DartCache, q, k_pool, v_pool, out, ws, *, scale: float, causal: bool = True, lse=None,
+                     status=None, stream=None):
+    """dart_attend over pools held in 4 bits."""
+    kind, Hq, _, d, T = cache._heads
+    qp, q_ld = _rows(q, kind, T, Hq, d, "q")
+    o, o_ld = _rows(out, kind, T, Hq, d, "out")
+    kc, ks = _codes(cache, k_pool, "k_pool")
+    vc, vs = _codes(cache, v_pool, "v_pool")
+    le, st = _plain(lse, T, Hq, "lse"), _status(status)
+    if T == 0:
+        return
+    rc = (_lib or lib()).dart_attend_4bit(cache._ref, qp, q_ld, kc, ks, vc, vs, scale, causal, o, o_ld, le, ws.data_ptr(),
+                                          ws.numel(), st, _stream(stream))
+    if rc:
+        _check(rc, "dart_attend_4bit")
+
+
+# ---- eviction ---------------------------------------------------------------------------------
+
+
+def _gathered(cache: DartCache, w, what: str):
+    """The address of the weights of a cache's keys: contiguous float32 [pages, Hkv, page_size]."""
+    if w.dtype is not torch.float32 or w.shape != cache._pool[0][:3] or not w.is_contiguous():
+        raise ValueError(f"{what}: contiguous float32 {tuple(cache._pool[0][:3])}")
+    return w.data_ptr()
+
+
+def dart_attend_weights_workspace_bytes(cache: DartCache) -> int:
+    return int(lib().dart_attend_weights_workspace_bytes(C.byref(cache), cache._scales is not None))
+
+
+def alloc_attend_weights_workspace(cache: DartCache, device="cuda") -> torch.Tensor:
+    return _workspace(dart_attend_weights_workspace_bytes(cache), "dart_attend_weights_workspace_bytes", device)
+
+
+def dart_attend_weights(cache: DartCache, q, k_pool, lse, weights, ws, *, scale: float, causal: bool = True, carry: float = 1.0,
+                        status=None, stream=None):
+    """weights (float32 [pages, Hkv, page_size]) of every key: carry times what they were, and what the tokens' queries
+    q [T, Hq*d] with the lse [T, Hq] of dart_attend give it.  Keys of the call's tokens start from 0.  k_pool: rows, or (codes, scales)
+    of a cache of make_cache_4bit."""
+    kind, Hq, _, d, T = cache._heads
+    qp, q_ld = _rows(q, kind, T, Hq, d, "q")
+    kp, ks = _held(cache, k_pool, "k_pool")
+    if lse is None:
+        raise ValueError("lse: as of dart_attend")
+    le, w, st = _plain(lse, T, Hq, "lse"), _gathered(cache, weights, "weights"), _status(status)
+    if T == 0:
+        return
+    rc = (_lib or lib()).dart_attend_weights(cache._ref, qp, q_ld, kp, ks, le, scale, causal, carry, w, ws.data_ptr(), ws.numel(),
+                                             st, _stream(stream))
+    if rc:
+        _check(rc, "dart_attend_weights")
+
+
+def make_eviction(*, budget: int = 0, ratio=(0, 1), first: int = 0, recent: int = 0) -> DartEviction:
+    """Keys that a sequence keeps: `budget`, or ratio[0]/ratio[1] of its keys where that is 0; the first and the recent ones
+    always."""
+    e = DartEviction()
+    e.budget, e.ratio_num, e.ratio_den, e.first, e.recent = budget, ratio[0], ratio[1], first, recent
+    e._ref = C.byref(e)
+    return e
+
+
+def dart_evict_most(cache: DartCache, eviction: DartEviction) -> int:
+    """Keys that a sequence keeps at most (entries of a row of `kept`)."""
+    n = int(lib().dart_evict_most(C.byref(cache), C.byref(eviction), cache._scales is not None))
+    if n < 0:
+        raise DartError(DART_ERR_SHAPE, "dart_evict_most")
+    return n
+
+
+def dart_evict_workspace_bytes(cache: DartCache, eviction: DartEviction) -> int:
+    return int(lib().dart_evict_workspace_bytes(C.byref(cache), C.byref(eviction), cache._scales is not None))
+
+
+def alloc_evict_workspace(cache: DartCache, eviction: DartEviction, device="cuda") -> torch.Tensor:
+    return _workspace(dart_evict_workspace_bytes(cache, eviction), "dart_evict_workspace_bytes", device)
+
+
+def dart_evict(cache: DartCache, eviction: DartEviction, k_pool, v_pool, weights, kv_len_out, ws, *, weights_out=None, kept=None,
+               status=None, stream=None):
+    """Every sequence cut to the keys of largest weight, moved to the front of its pages; kv_len_out int32 [B] (may be the
+    kv_len of the cache), weights_out like weights (may be weights), kept int32 [B, Hkv, n]: the places they had."""
+    kp, ks = _held(cache, k_pool, "k_pool")
+    vp, vs = _held(cache, v_pool, "v_pool")
+    w, w_out = _gathered(cache, weights, "weights"), None if weights_out is None else _gathered(cache, weights_out, "weights_out")
+    if kv_len_out.dtype is not torch.int32 or kv_len_out.numel() != cache.B or not kv_len_out.is_contiguous():
+        raise ValueError(f"kv_len_out: contiguous int32 [{cache.B}]")
+    at, ld = None, 0
+    if kept is not None:
+        if kept.dtype is not torch.int32 or kept.dim() != 3 or kept.shape[:2] != (cache.B, cache.Hkv) or not kept.is_contiguous():
+            raise ValueError(f"kept: contiguous int32 [{cache.B}, {cache.Hkv}, n]")
+        at, ld = kept.data_ptr(), kept.shape[2]
+    st = _status(status)
+    if cache.B == 0:
+        return
+    rc = (_lib or lib()).dart_evict(cache._ref, eviction._ref, kp, ks, vp, vs, w, w_out, at, ld, kv_len_out.data_ptr(), ws.data_ptr(),
+                                    ws.numel(), st, _stream(stream))
+    if rc:
+        _check(rc, "dart_evict")

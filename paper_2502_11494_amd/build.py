@@ -18,7 +18,7 @@ from concurrent.futures import ThreadPoolExecutor
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
-SOURCES = ("dart_api.hip", "attend_api.hip")  # translation units, compiled side by side
+SOURCES = ("dart_api.hip", "attend_api.hip", "fourbit_api.hip", "evict_api.hip")  # translation units, compiled side by side
 LIB = os.path.join(_HERE, "libdart_hip.so")  # the path binding.py loads
 STAMP = LIB + ".sha256"
 

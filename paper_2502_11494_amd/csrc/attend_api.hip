@@ -14,89 +14,6 @@ using namespace dart;
 
 namespace {
 
-constexpr size_t kAlign = 256;
-constexpr int64_t kMaxLd = int64_t(1) << 24;       // row strides of q, k, v and outputs, elements
-constexpr int64_t kMaxPoolLd = int64_t(1) << 33;   // strides inside the pools, elements: 16-byte units fit 32 bits
-constexpr int kMaxSequences = 1 << 20, kMaxTokens = 1 << 24, kMaxKeys = 1 << 27, kMaxPage = 1 << 20;
-constexpr int kMaxHeads = 1024, kMaxHead = 256;
-constexpr long kJoinSets = 1L << 15;  // sets of lanes of a join that fill the chip
-constexpr long kMaxJoined = 1L << 24;  // (token, query head) pairs whose parts are joined
-constexpr long kMaxRows = 1L << 28, kMaxBlocks = (1L << 23) - 1;  // (token, head) pairs of a key head; blocks of a launch
-
-inline bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-inline int elem(int dtype) { return dtype == DART_BF16 ? 2 : 4; }
-
-#define DART_TRY(expr)                    \
-  do {                                    \
-    dart_status _s = (expr);              \
-    if (_s != DART_OK) return _s;         \
-  } while (0)
-
-dart_status launched() { return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP; }
-
-dart_status check_heads(int Hq, int Hkv, int d, int dtype) {
-  if (dtype != DART_F32 && dtype != DART_BF16) return DART_ERR_DTYPE;
-  if (Hkv < 1 || Hq < Hkv || Hq > kMaxHeads || Hq % Hkv || d < 8 || d > kMaxHead || d % 8) return DART_ERR_SHAPE;
-  return DART_OK;
-}
-
-// A tensor of rows of `width` elements.
-dart_status check_rows(const void* p, int64_t ld, int64_t width, int dtype) {
-  if (!p) return DART_ERR_NULL;
-  if (ld < width || ld > kMaxLd) return DART_ERR_SHAPE;
-  if (off16(p) || ld * elem(dtype) % 16) return DART_ERR_ALIGN;
-  return DART_OK;
-}
-
-dart_status make_cache(const dart_cache* u, Cache& c) {
-  if (!u) return DART_ERR_NULL;
-  DART_TRY(check_heads(u->Hq, u->Hkv, u->d, u->dtype));
-  if (u->B < 0 || u->B > kMaxSequences || u->T < 0 || u->T > kMaxTokens || u->max_q < 0 || u->max_kv < 0 ||
-      u->max_kv > kMaxKeys || u->pages_ld < 1 || u->pages_n < 0 || u->n_pages < 1)
-    return DART_ERR_SHAPE;
-  if (u->page_size < 1 || u->page_size > kMaxPage || (u->page_size & (u->page_size - 1))) return DART_ERR_SHAPE;
-  if (u->row_ld < u->d || u->row_ld > kMaxPoolLd || u->head_ld < 0 || u->head_ld > kMaxPoolLd || u->page_ld < 0 ||
-      u->page_ld > kMaxPoolLd)
-    return DART_ERR_SHAPE;
-  if (u->groups < 0 || u->groups > u->B) return DART_ERR_SHAPE;
-  if (!u->cu_q && u->T != u->B) return DART_ERR_SHAPE;
-  const int64_t a16 = 16 / elem(u->dtype);
-  if (u->row_ld % a16 || u->head_ld % a16 || u->page_ld % a16) return DART_ERR_ALIGN;
-  c = {};
-  c.B = u->B;
-  c.Hq = u->Hq;
-  c.Hkv = u->Hkv;
-  c.d = u->d;
-  c.T = u->T;
-  c.max_q = u->cu_q ? std::min(u->max_q, u->T) : 1;
-  c.max_kv = u->max_kv;
-  c.cu = u->cu_q;
-  c.kv_len = u->kv_len;
-  c.pages = u->pages;
-  c.pages_ld = u->pages_ld;
-  c.pages_n = u->pages_n ? u->pages_n : u->pages_ld;
-  c.n_pages = u->n_pages;
-  c.page_shift = __builtin_ctz((unsigned)u->page_size);
-  c.page_ld = u->page_ld;
-  c.head_ld = u->head_ld;
-  c.row_ld = u->row_ld;
-  c.page_16 = (uint32_t)(u->page_ld / a16);
-  c.row_16 = (uint32_t)(u->row_ld / a16);
-  c.groups = u->groups;
-  if (u->groups > 0) {
-    if (u->max_prefix < 0 || u->max_prefix > kMaxKeys || u->prefix_ld < 1 || u->prefix_n < 0) return DART_ERR_SHAPE;
-    if (!u->group_cu || !u->prefix_pages || !u->prefix_len) return DART_ERR_NULL;
-    c.max_prefix = u->max_prefix;
-    c.prefix_ld = u->prefix_ld;
-    c.prefix_n = u->prefix_n ? u->prefix_n : u->prefix_ld;
-    c.group_cu = u->group_cu;
-    c.prefix_pages = u->prefix_pages;
-    c.prefix_len = u->prefix_len;
-  }
-  if (u->B > 0 && (!u->kv_len || !u->pages)) return DART_ERR_NULL;
-  return DART_OK;
-}
-
 dart_status make_rotate(const dart_rotation* u, Rotate& a) {
   if (!u) return DART_ERR_NULL;
   DART_TRY(check_heads(u->Hq, u->Hkv, u->d, u->dtype));
@@ -176,89 +93,6 @@ dart_status set_rows(Rotate& a, int dtype, int T, const void* q, int64_t q_ld, c
   return DART_OK;
 }
 
-// ---- attention: which tiles, how many parts ---------------------------------------------------
-enum Kind { kFew, kMany, kWide };  // 16 rows, the keys dealt to four waves; four waves of rows; eight
-
-struct AttendPlan {
-  Kind own_kind, pre_kind;
-  Parting own, pre;
-  bool both;  // one launch takes the prefixes and the own keys
-  int parts;
-  size_t o_ml, total;
-};
-
-int rows_of(Kind k, int dtype, int d) { return k == kFew ? 16 : k == kWide ? 256 : 4 * many_columns(dtype == DART_BF16 ? kBF16 : kF32, d); }
-long blocks_of(const Cache& c, const Parting& p) { return p.slots * c.Hkv * p.chunks; }
-
-// rows: (token, head) pairs of a sequence at most, of a group on average (nothing on the host says how many sequences the
-// largest has); owners: how many of them.  Uneven groups read their prefix in smaller tiles than they could: 64 answers of 32 heads
-// over four prefixes of 2880 53 us with 16 sequences to each, 65 with 61, 1, 1 and 1.  max_keys: the caller's bound, which
-// divides the keys, whatever the lengths are: one token over 2000 keys, 28 + 4 heads, 12.4 us, 27 with a bound of 131 072; 32 of
-// them 28 and 44.
-Kind plan_parting(const Cache& c, int dtype, bool prefix, long rows, int owners, int max_keys, Parting& p) {
-  const int r = c.Hq / c.Hkv;
-  // 256-row tiles take the least from LDS and caches per row, but each has a compute unit to itself, so that nothing
-  // hides its start and end: they pay from 1024 keys and 1.5 tiles to a unit on.  28 + 4 heads, causal, 128- and
-  // 256-row tiles: two sequences of 9216 1347 and 1258 us, one of 4096 159 and 136, one of 3600 124 and 116, one of 2048
-  // 58 and 66; 24 of 1000 291 and 283, 16 of 600 91 and 95.
-  const bool wide = dtype == DART_BF16 && c.d <= 128 && rows > 128 && max_keys >= 1024 && (long)c.T * r / 256 * c.Hkv >= 384;
-  // 16-row tiles with the keys dealt to four waves end sooner while the chip is not full (256 units of 384 keys):
-  // one sequence of 9 tokens over 300 keys, 28 + 4 heads, 11.7 us and 14.1 in 128-row tiles, over 3000 keys 13.4 and 16.2;
-  // 32 such sequences 89 and 63.  Up to 16 rows nothing is gained by reading for more.
-  const long few = std::min((long)c.T * r / 16 + owners, (long)owners * ((rows + 15) / 16)) * c.Hkv;
-  Kind kind = rows <= 16 || (rows <= 64 && few * max_keys <= 256 * 384) ? kFew : wide ? kWide : kMany;
-  if (dtype == DART_F32 && c.d > 128) kind = kMany;
-  const int bm = rows_of(kind, dtype, c.d);
-  p = {};
-  p.prefix = prefix;
-  p.few = kind == kFew;
-  if (!prefix && !c.cu) {
-    p.per_owner = (r + bm - 1) / bm;
-    p.slots = (long)owners * p.per_owner;
-  } else {
-    p.slots = (long)c.T * r / bm + owners;
-  }
-  const long blocks = std::max(1L, std::min(p.slots, (long)owners * ((rows + bm - 1) / bm)) * c.Hkv);
-  // Parts until every compute unit has a block, of 256 keys at least; more cost their start (7 us a round) and the
-  // join: 64 rows of 28 + 4 heads over 8000 keys 197 us in one part, 40 in 128 blocks, 31 in 256, 33 in 512, 46 in
-  // 1024; 64 answers over one prefix of 9216 229, 43, 34, 42 and 48.  32-bit tiles of four waves are bound by the
-  // matrix cores' latency and want company: 637 causal tokens of 32 heads 69 us in 320 blocks, 58 in 960.
-  const long want = std::max(1L, (dtype == DART_F32 && kind == kMany ? 1024 : 256) / blocks);
-  const long chunk = std::max(256L, ((max_keys + want - 1) / want + 255) / 256 * 256);
-  p.chunk = (int)chunk;
-  p.chunks = std::max(1, (int)((max_keys + chunk - 1) / chunk));
-  return kind;
-}
-
-dart_status plan_attend(const Cache& c, int dtype, AttendPlan& p) {
-  const int r = c.Hq / c.Hkv;
-  if ((long)c.T * r > kMaxRows) return DART_ERR_SHAPE;
-  p = {};
-  p.own_kind = plan_parting(c, dtype, false, (long)c.max_q * r, c.B, c.max_kv, p.own);
-  p.parts = p.own.chunks;
-  if (c.groups > 0) {
-    const long rows = std::min((long)c.T, (long)c.max_q * c.B) * r;
-    p.pre_kind = plan_parting(c, dtype, true, std::max(1L, (rows + c.groups - 1) / c.groups), c.groups, c.max_prefix, p.pre);
-    p.parts += p.pre.chunks;
-    p.own.first_part = p.pre.chunks;
-    // One launch for both: 64 answers over a prefix of 9216 keys, 28 + 4 heads, 33 us and 44 in two, 32 prompts over four of 2880
-    // 126 and 143.  With 32-bit rows it takes the registers of two blocks, which costs more than a launch where there are
-    // blocks enough: 16 answers over two prefixes of 3000, 64 + 8 heads (320 blocks), 50 and 69; those 64 answers (1264) 149 and 129.
-    p.both = p.own_kind != kWide && p.pre_kind != kWide && blocks_of(c, p.own) + blocks_of(c, p.pre) <= kMaxBlocks &&
-             (dtype == DART_BF16 || (c.d <= 128 && blocks_of(c, p.own) + blocks_of(c, p.pre) <= 1024));
-  }
-  if (p.parts > 1 && (long)c.T * c.Hq > kMaxJoined) return DART_ERR_SHAPE;
-  p.own.parts = p.pre.parts = p.parts;
-  auto up = [](size_t v) { return (v + kAlign - 1) / kAlign * kAlign; };
-  const size_t rows = (size_t)c.T * c.Hq;
-  p.total = kAlign;
-  if (p.parts > 1) {
-    p.o_ml = up((size_t)p.parts * rows * c.d * 4);
-    p.total = p.o_ml + up((size_t)p.parts * rows * 8);
-  }
-  return DART_OK;
-}
-
 template <int DT, int DP, int QW, int WM, int WK, int KT>
 dart_status launch_tiles(const Attend& a, const Cache& c, const Parting& sp, hipStream_t st) {
   typedef AttendShape<DT, DP, QW, WM, WK, KT> S;
@@ -304,6 +138,21 @@ dart_status launch_attend(const Attend& a, const Cache& c, int dtype, const Part
 }
 
 }  // namespace
+
+namespace dart {
+
+dart_status dart_attend_join(const Attend& a, const Cache& c, int dtype, const AttendPlan& p, hipStream_t st) {
+  const JoinPlan j = plan_join(c, p.parts);
+  if (dtype == DART_BF16)
+    k_attend_join<kBF16><<<dim3((unsigned)j.blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, p.own.part_o,
+                                                                        p.own.part_ml, j.lanes_shift, j.split_shift);
+  else
+    k_attend_join<kF32><<<dim3((unsigned)j.blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, p.own.part_o,
+                                                                       p.own.part_ml, j.lanes_shift, j.split_shift);
+  return launched();
+}
+
+}  // namespace dart
 
 extern "C" {
 
@@ -385,19 +234,7 @@ dart_status dart_attend(const dart_cache* cache, const void* q, int64_t q_ld, co
     DART_TRY(launch_attend(a, c, cache->dtype, p.own, p.own_kind, st));
   }
   if (p.parts == 1) return DART_OK;
-  int lanes_shift = 0, split_shift = 0;
-  while ((4 << lanes_shift) < c.d) ++lanes_shift;
-  // many parts of few rows are shared by up to a block's sets of lanes, four parts at least to each
-  while (split_shift < 8 - lanes_shift && (4 << split_shift) < p.parts && ((long)c.T * c.Hq << split_shift) < kJoinSets) ++split_shift;
-  const int rows_shift = 8 - lanes_shift - split_shift;
-  const long blocks = (((long)c.T * c.Hq - 1) >> rows_shift) + 1;
-  if (bf16)
-    k_attend_join<kBF16><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, part_o, part_ml,
-                                                                      lanes_shift, split_shift);
-  else
-    k_attend_join<kF32><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, part_o, part_ml,
-                                                                     lanes_shift, split_shift);
-  return launched();
+  return dart_attend_join(a, c, cache->dtype, p, st);
 }
 
 }  // extern "C"

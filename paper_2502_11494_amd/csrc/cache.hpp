@@ -1,6 +1,9 @@
 // The paged cache as kernels see it, and the checks every one of them makes the same way.
 #pragma once
 
+#include <algorithm>
+
+#include "../../include/dart.h"
 #include "common.hpp"
 
 namespace dart {
@@ -77,6 +80,91 @@ __device__ __forceinline__ long key_offset(const Cache& c, const int* table, int
   const int page = table[key >> c.page_shift];
   bad = (unsigned)page >= (unsigned)c.n_pages;
   return (bad ? 0L : (long)page * c.page_ld) + (long)(key & ((1 << c.page_shift) - 1)) * c.row_ld;
+}
+
+// ---- host: limits and checks of descriptors and tensors ------------------------------------
+constexpr size_t kAlign = 256;
+constexpr int64_t kMaxLd = int64_t(1) << 24;       // row strides of q, k, v and outputs, elements
+constexpr int64_t kMaxPoolLd = int64_t(1) << 33;   // strides inside the pools, elements: 16-byte units fit 32 bits
+constexpr int kMaxSequences = 1 << 20, kMaxTokens = 1 << 24, kMaxKeys = 1 << 27, kMaxPage = 1 << 20;
+constexpr int kMaxHeads = 1024, kMaxHead = 256;
+constexpr long kJoinSets = 1L << 15;  // sets of lanes of a join that fill the chip
+constexpr long kMaxJoined = 1L << 24;  // (token, query head) pairs whose parts are joined
+constexpr long kMaxRows = 1L << 28, kMaxBlocks = (1L << 23) - 1;  // (token, head) pairs of a key head; blocks of a launch
+
+inline bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+inline int elem(int dtype) { return dtype == DART_BF16 ? 2 : 4; }
+
+#define DART_TRY(expr)                    \
+  do {                                    \
+    dart_status _s = (expr);              \
+    if (_s != DART_OK) return _s;         \
+  } while (0)
+
+inline dart_status launched() { return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP; }
+
+inline dart_status check_heads(int Hq, int Hkv, int d, int dtype) {
+  if (dtype != DART_F32 && dtype != DART_BF16) return DART_ERR_DTYPE;
+  if (Hkv < 1 || Hq < Hkv || Hq > kMaxHeads || Hq % Hkv || d < 8 || d > kMaxHead || d % 8) return DART_ERR_SHAPE;
+  return DART_OK;
+}
+
+// A tensor of rows of `width` elements.
+inline dart_status check_rows(const void* p, int64_t ld, int64_t width, int dtype) {
+  if (!p) return DART_ERR_NULL;
+  if (ld < width || ld > kMaxLd) return DART_ERR_SHAPE;
+  if (off16(p) || ld * elem(dtype) % 16) return DART_ERR_ALIGN;
+  return DART_OK;
+}
+
+// bits: 4 where the pools are held in 4 bits, in whole blocks of 32 values; otherwise their rows are of u->dtype.
+inline dart_status make_cache(const dart_cache* u, Cache& c, int bits = 0) {
+  if (!u) return DART_ERR_NULL;
+  DART_TRY(check_heads(u->Hq, u->Hkv, u->d, u->dtype));
+  if (u->B < 0 || u->B > kMaxSequences || u->T < 0 || u->T > kMaxTokens || u->max_q < 0 || u->max_kv < 0 ||
+      u->max_kv > kMaxKeys || u->pages_ld < 1 || u->pages_n < 0 || u->n_pages < 1)
+    return DART_ERR_SHAPE;
+  if (u->page_size < 1 || u->page_size > kMaxPage || (u->page_size & (u->page_size - 1))) return DART_ERR_SHAPE;
+  if (u->row_ld < (bits == 4 ? (u->d + 31) / 32 * 32 : u->d) || u->row_ld > kMaxPoolLd || u->head_ld < 0 || u->head_ld > kMaxPoolLd || u->page_ld < 0 ||
+      u->page_ld > kMaxPoolLd)
+    return DART_ERR_SHAPE;
+  if (u->groups < 0 || u->groups > u->B) return DART_ERR_SHAPE;
+  if (!u->cu_q && u->T != u->B) return DART_ERR_SHAPE;
+  const int64_t a16 = bits == 4 ? 32 : 16 / elem(u->dtype);
+  if (u->row_ld % a16 || u->head_ld % a16 || u->page_ld % a16) return DART_ERR_ALIGN;
+  c = {};
+  c.B = u->B;
+  c.Hq = u->Hq;
+  c.Hkv = u->Hkv;
+  c.d = u->d;
+  c.T = u->T;
+  c.max_q = u->cu_q ? std::min(u->max_q, u->T) : 1;
+  c.max_kv = u->max_kv;
+  c.cu = u->cu_q;
+  c.kv_len = u->kv_len;
+  c.pages = u->pages;
+  c.pages_ld = u->pages_ld;
+  c.pages_n = u->pages_n ? u->pages_n : u->pages_ld;
+  c.n_pages = u->n_pages;
+  c.page_shift = __builtin_ctz((unsigned)u->page_size);
+  c.page_ld = u->page_ld;
+  c.head_ld = u->head_ld;
+  c.row_ld = u->row_ld;
+  c.page_16 = (uint32_t)(u->page_ld / a16);
+  c.row_16 = (uint32_t)(u->row_ld / a16);
+  c.groups = u->groups;
+  if (u->groups > 0) {
+    if (u->max_prefix < 0 || u->max_prefix > kMaxKeys || u->prefix_ld < 1 || u->prefix_n < 0) return DART_ERR_SHAPE;
+    if (!u->group_cu || !u->prefix_pages || !u->prefix_len) return DART_ERR_NULL;
+    c.max_prefix = u->max_prefix;
+    c.prefix_ld = u->prefix_ld;
+    c.prefix_n = u->prefix_n ? u->prefix_n : u->prefix_ld;
+    c.group_cu = u->group_cu;
+    c.prefix_pages = u->prefix_pages;
+    c.prefix_len = u->prefix_len;
+  }
+  if (u->B > 0 && (!u->kv_len || !u->pages)) return DART_ERR_NULL;
+  return DART_OK;
 }
 
 }  // namespace dart

@@ -1,6 +1,8 @@
 // Attention over the paged cache: tiles of query rows against tiles of keys on the matrix cores.
 #pragma once
 
+#include <type_traits>
+
 #include "cache.hpp"
 #include "k_rotate.hpp"
 
@@ -27,6 +29,7 @@ struct Attend {
   float scale;
   int causal;
   double per_token;  // 1 / (rows of a token: query heads of a key head)
+  const uint8_t *k_scales, *v_scales;  // (keys and values held in 4 bits: their pools are codes, these the blocks' scales)
 };
 
 // row / rows of a token, exactly: rows are below 2^28.
@@ -173,14 +176,22 @@ __device__ __forceinline__ int slot_owner(const Cache& c, const int* group_cu, i
   }
 }
 
-// WM waves along the rows, QW each, by WK along the keys; a step takes KT keys per key group.
-template <int DT, int DP, int QW, int WM, int WK, int KT>
+// Pools of rows of the queries' type: loads of 16 bytes.
+struct AsRows {
+  static constexpr bool kCodes = false;
+  static constexpr int unit(int piece, int) { return piece; }
+};
+
+// WM waves along the rows, QW each, by WK along the keys; a step takes KT keys per key group.  HELD: how the
+// pools hold keys and values (they go to LDS in the type of the rows).
+template <int DT, int DP, int QW, int WM, int WK, int KT, class HELD = AsRows>
 struct AttendShape {
   static constexpr int kEsz = DT == kBF16 ? 2 : 4;
   static constexpr int kRowBytes = DP * kEsz;
-  static constexpr int kPieces = kRowBytes / 16;
   static constexpr int kThreads = 64 * WM * WK;
   static constexpr int kGroup = 64 * WM;                 // threads that stage a key group's tiles
+  static constexpr int kUnit = HELD::unit(16 / kEsz, KT * DP / kGroup);  // values of a load
+  static constexpr int kPieces = DP / kUnit;             // loads of a row
   static constexpr int kLoads = KT * kPieces / kGroup;   // pieces of keys (and of values) per thread
   static constexpr int kApart = kGroup / kPieces;        // rows between a thread's pieces
   static constexpr int kBuffers = WM > 1 ? 2 : 1;
@@ -195,6 +206,12 @@ struct AttendShape {
 // Columns of a wave's tile where four waves take the rows: 32 halve what LDS has to deliver per product, but with
 // 32-bit rows the matrix cores are what counts, and with heads over 128 the registers are.
 constexpr int many_columns(int dt, int d) { return dt == kBF16 && d <= 128 ? 32 : 16; }
+
+// What one load brings: a piece of a row, or words of codes.
+template <int WORDS>
+struct Codes {
+  uint32_t v[WORDS];
+};
 
 // What a block keeps in LDS beside the tiles.
 struct AttendShared {
@@ -216,10 +233,10 @@ struct AttendShared {
 // 32-bit rows, the matrix cores' rate (637 causal tokens of 32 heads 55 us with the join's 8,
 // the matrix cores busy for 22; 4096 tokens of 28 + 4 heads 1.07 ms, 112 TFLOP/s of the 153 of a large product).
 // One block: row tile `slot` against chunk `part` of the keys of head `head`.
-template <int DT, int DP, int QW, int WM, int WK, int KT>
+template <int DT, int DP, int QW, int WM, int WK, int KT, class HELD = AsRows>
 __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, const Parting& sp, unsigned char* lds, AttendShared& sh,
                                             long slot, int head, int part) {
-  typedef AttendShape<DT, DP, QW, WM, WK, KT> S;
+  typedef AttendShape<DT, DP, QW, WM, WK, KT, HELD> S;
   typedef Math<DT, QW> M;
   typedef typename M::acc acc;
   constexpr int kSteps = M::template steps<DP>(), kDT = DP / QW, kSub = KT / 32, RB = S::kRowBytes;
@@ -277,13 +294,18 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   // past the keys (or the head) is read again from the last of them, and put right as it goes to LDS.
   const int gt = threadIdx.x - wk * S::kGroup;
   const int my_row = gt / S::kPieces, my_piece = gt % S::kPieces;
-  const bool my_on = my_piece * M::kVec < c.d;
-  const long piece_at = ((long)head * c.head_ld + (my_on ? my_piece * M::kVec : 0)) * S::kEsz;
+  const bool my_on = my_piece * S::kUnit < c.d;
+  const long my_at = (long)head * c.head_ld + (my_on ? my_piece * S::kUnit : 0);
+  const long piece_at = HELD::kCodes ? my_at / 2 : my_at * S::kEsz;
   const unsigned char* kp = static_cast<const unsigned char*>(a.k_pool) + piece_at;
   const unsigned char* vp = static_cast<const unsigned char*>(a.v_pool) + piece_at;
+  const uint8_t* ks = HELD::kCodes ? a.k_scales + my_at / 32 : nullptr;
+  const uint8_t* vs = HELD::kCodes ? a.v_scales + my_at / 32 : nullptr;
   unsigned char* const my_lds = lds + wk * (S::kBuffers * 2 * S::kTileBytes);
   const int row_mask = (1 << c.page_shift) - 1, last_key = k1 - 1;
-  u32x4 kr[S::kLoads], vr[S::kLoads];
+  typedef typename std::conditional<HELD::kCodes, Codes<S::kUnit / 8 ? S::kUnit / 8 : 1>, u32x4>::type Load;
+  Load kr[S::kLoads], vr[S::kLoads];
+  uint32_t ke[S::kLoads], ve[S::kLoads];  // (scales)
   int pg[S::kLoads];
   bool bad_page = false;
   auto load_pages = [&](int kb) {
@@ -295,14 +317,18 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     int page = pg[i];
     if ((unsigned)page >= (unsigned)c.n_pages) page = 0, bad_page = true;
     const uint32_t row = min(kb + my_row + i * S::kApart, last_key) & row_mask;
-    return ((uint64_t)(uint32_t)page * c.page_16 + (uint64_t)row * c.row_16) << 4;
+    return (uint64_t)(uint32_t)page * c.page_16 + (uint64_t)row * c.row_16;
   };
   auto load_tile = [&](int kb) {
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
       const uint64_t off = place_of(i, kb);
-      kr[i] = *reinterpret_cast<const u32x4*>(kp + off);
-      vr[i] = *reinterpret_cast<const u32x4*>(vp + off);
+      __builtin_memcpy(&kr[i], __builtin_assume_aligned(kp + (off << 4), sizeof(Load)), sizeof(Load));
+      __builtin_memcpy(&vr[i], __builtin_assume_aligned(vp + (off << 4), sizeof(Load)), sizeof(Load));
+      if constexpr (HELD::kCodes) {
+        ke[i] = ks[off];
+        ve[i] = vs[off];
+      }
     }
   };
   const int steps = (k1 - k0 + KT * WK - 1) / (KT * WK);
@@ -332,33 +358,45 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   const int lim_last = row0 + wm * QW < rows ? __builtin_amdgcn_readlane(lim, 63) : -1;   // (none: no key)
   const int lim_block = causal ? min(kv - n + token_in(a, row0), last_key) : last_key;    // of the block's
 
+  // Load i of a thread to its 16-byte pieces of a tile's row.
+  auto store_row = [&](unsigned char* to, int i, const Load& x, uint32_t scale, bool on) {
+    constexpr int kSplit = S::kUnit / M::kVec;
+    const int row = my_row + i * S::kApart;
+#pragma unroll
+    for (int j = 0; j < kSplit; ++j) {
+      u32x4 v;
+      if constexpr (HELD::kCodes) v = HELD::template piece<DT>(x.v[j * M::kVec / 8], scale, j * M::kVec / 4 % 2);
+      else v = x;
+      *reinterpret_cast<u32x4*>(to + row * RB + (((my_piece * kSplit + j) ^ mix<RB>(row)) << 4)) = on ? v : u32x4{0, 0, 0, 0};
+    }
+  };
   auto store_keys = [&](unsigned char* to) {
 #pragma unroll
-    for (int i = 0; i < S::kLoads; ++i) {
-      const int row = my_row + i * S::kApart;
-      *reinterpret_cast<u32x4*>(to + row * RB + ((my_piece ^ mix<RB>(row)) << 4)) = my_on ? kr[i] : u32x4{0, 0, 0, 0};
-    }
+    for (int i = 0; i < S::kLoads; ++i) store_row(to, i, kr[i], ke[i], my_on);
   };
   auto store_values = [&](unsigned char* to, int kb) {
     if (kb + KT > k1) {
       // What lies behind the keys may be anything; its weight is 0, and 0 times NaN is NaN.
 #pragma unroll
       for (int i = 0; i < S::kLoads; ++i)
-        if (kb + my_row + i * S::kApart >= k1) vr[i] = u32x4{0, 0, 0, 0};
+        if (kb + my_row + i * S::kApart >= k1) vr[i] = Load{}, ve[i] = 0;
     }
     if (kb + KT - 1 > lim_block && causal) {
       // Some row does not see some of these keys.  Their weight is 0 there, but its product with a value
       // that is no number would be none either: such values are left out here and added at the end.
       uint32_t odd = 0;
 #pragma unroll
-      for (int i = 0; i < S::kLoads; ++i) odd |= drop_infinities<DT>(vr[i]);
+      for (int i = 0; i < S::kLoads; ++i) {
+        if constexpr (HELD::kCodes) {
+          if (HELD::no_number(ve[i])) vr[i] = Load{}, ve[i] = 0, odd = 1;
+        } else {
+          odd |= drop_infinities<DT>(vr[i]);
+        }
+      }
       if (odd) sh.odd_values[wk] = 1;
     }
 #pragma unroll
-    for (int i = 0; i < S::kLoads; ++i) {
-      const int row = my_row + i * S::kApart;
-      *reinterpret_cast<u32x4*>(to + row * RB + ((my_piece ^ mix<RB>(row)) << 4)) = vr[i];
-    }
+    for (int i = 0; i < S::kLoads; ++i) store_row(to, i, vr[i], ve[i], true);
   };
 
   // This lane's share of its query's result, four elements of the head at a time: quad number x is elements
@@ -541,7 +579,10 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
         for (int s = 0; s < kSteps; ++s) {
           const int e = (M::kGroups * s + grp) * M::kVec;
           Piece<DT, M::kVec> kf = {}, qf;
-          if (e < c.d) kf = load_piece<DT, M::kVec>(a.k_pool, at + e);
+          if (e < c.d) {
+            if constexpr (HELD::kCodes) kf = HELD::template values<DT, M::kVec>(a.k_pool, a.k_scales, at + e);
+            else kf = load_piece<DT, M::kVec>(a.k_pool, at + e);
+          }
           __builtin_memcpy(&qf, &q[s], 16);
 #pragma unroll
           for (int j = 0; j < M::kVec; ++j) w = fmaf(qf.get(j), kf.get(j), w);
@@ -551,7 +592,10 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
         if (key > lim) continue;
 #pragma unroll
         for (int x = 0; x < kQuads; ++x) {
-          const Piece<DT, 4> v = load_piece<DT, 4>(a.v_pool, at + min(quad_at(x), c.d - 4));  // (past the head: not stored)
+          const long from = at + min(quad_at(x), c.d - 4);  // (past the head: not stored)
+          Piece<DT, 4> v;
+          if constexpr (HELD::kCodes) v = HELD::template values<DT, 4>(a.v_pool, a.v_scales, from);
+          else v = load_piece<DT, 4>(a.v_pool, from);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             if (fabsf(v.get(k)) < INFINITY) continue;
@@ -787,5 +831,107 @@ __global__ __launch_bounds__(256) void k_attend_join(Attend a, Cache c, int pre_
   const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
   store_piece<DT, 4>(a.out, (long)t * a.out_ld + (long)h * c.d + e, round_piece<DT, 4>(y));
 }
+
+// ---- attention: which tiles, how many parts ---------------------------------------------------
+enum Kind { kFew, kMany, kWide };  // 16 rows, the keys dealt to four waves; four waves of rows; eight
+
+struct AttendPlan {
+  Kind own_kind, pre_kind;
+  Parting own, pre;
+  bool both;  // one launch takes the prefixes and the own keys
+  int parts;
+  size_t o_ml, total;
+};
+
+inline int rows_of(Kind k, int dtype, int d) { return k == kFew ? 16 : k == kWide ? 256 : 4 * many_columns(dtype == DART_BF16 ? kBF16 : kF32, d); }
+inline long blocks_of(const Cache& c, const Parting& p) { return p.slots * c.Hkv * p.chunks; }
+
+// rows: (token, head) pairs of a sequence at most, of a group on average (nothing on the host says how many sequences the
+// largest has); owners: how many of them.  Uneven groups read their prefix in smaller tiles than they could: 64 answers of 32 heads
+// over four prefixes of 2880 53 us with 16 sequences to each, 65 with 61, 1, 1 and 1.  max_keys: the caller's bound, which
+// divides the keys, whatever the lengths are: one token over 2000 keys, 28 + 4 heads, 12.4 us, 27 with a bound of 131 072; 32 of
+// them 28 and 44.
+inline Kind plan_parting(const Cache& c, int dtype, bool prefix, long rows, int owners, int max_keys, Parting& p) {
+  const int r = c.Hq / c.Hkv;
+  // 256-row tiles take the least from LDS and caches per row, but each has a compute unit to itself, so that nothing
+  // hides its start and end: they pay from 1024 keys and 1.5 tiles to a unit on.  28 + 4 heads, causal, 128- and
+  // 256-row tiles: two sequences of 9216 1347 and 1258 us, one of 4096 159 and 136, one of 3600 124 and 116, one of 2048
+  // 58 and 66; 24 of 1000 291 and 283, 16 of 600 91 and 95.
+  const bool wide = dtype == DART_BF16 && c.d <= 128 && rows > 128 && max_keys >= 1024 && (long)c.T * r / 256 * c.Hkv >= 384;
+  // 16-row tiles with the keys dealt to four waves end sooner while the chip is not full (256 units of 384 keys):
+  // one sequence of 9 tokens over 300 keys, 28 + 4 heads, 11.7 us and 14.1 in 128-row tiles, over 3000 keys 13.4 and 16.2;
+  // 32 such sequences 89 and 63.  Up to 16 rows nothing is gained by reading for more.
+  const long few = std::min((long)c.T * r / 16 + owners, (long)owners * ((rows + 15) / 16)) * c.Hkv;
+  Kind kind = rows <= 16 || (rows <= 64 && few * max_keys <= 256 * 384) ? kFew : wide ? kWide : kMany;
+  if (dtype == DART_F32 && c.d > 128) kind = kMany;
+  const int bm = rows_of(kind, dtype, c.d);
+  p = {};
+  p.prefix = prefix;
+  p.few = kind == kFew;
+  if (!prefix && !c.cu) {
+    p.per_owner = (r + bm - 1) / bm;
+    p.slots = (long)owners * p.per_owner;
+  } else {
+    p.slots = (long)c.T * r / bm + owners;
+  }
+  const long blocks = std::max(1L, std::min(p.slots, (long)owners * ((rows + bm - 1) / bm)) * c.Hkv);
+  // Parts until every compute unit has a block, of 256 keys at least; more cost their start (7 us a round) and the
+  // join: 64 rows of 28 + 4 heads over 8000 keys 197 us in one part, 40 in 128 blocks, 31 in 256, 33 in 512, 46 in
+  // 1024; 64 answers over one prefix of 9216 229, 43, 34, 42 and 48.  32-bit tiles of four waves are bound by the
+  // matrix cores' latency and want company: 637 causal tokens of 32 heads 69 us in 320 blocks, 58 in 960.
+  const long want = std::max(1L, (dtype == DART_F32 && kind == kMany ? 1024 : 256) / blocks);
+  const long chunk = std::max(256L, ((max_keys + want - 1) / want + 255) / 256 * 256);
+  p.chunk = (int)chunk;
+  p.chunks = std::max(1, (int)((max_keys + chunk - 1) / chunk));
+  return kind;
+}
+
+inline dart_status plan_attend(const Cache& c, int dtype, AttendPlan& p) {
+  const int r = c.Hq / c.Hkv;
+  if ((long)c.T * r > kMaxRows) return DART_ERR_SHAPE;
+  p = {};
+  p.own_kind = plan_parting(c, dtype, false, (long)c.max_q * r, c.B, c.max_kv, p.own);
+  p.parts = p.own.chunks;
+  if (c.groups > 0) {
+    const long rows = std::min((long)c.T, (long)c.max_q * c.B) * r;
+    p.pre_kind = plan_parting(c, dtype, true, std::max(1L, (rows + c.groups - 1) / c.groups), c.groups, c.max_prefix, p.pre);
+    p.parts += p.pre.chunks;
+    p.own.first_part = p.pre.chunks;
+    // One launch for both: 64 answers over a prefix of 9216 keys, 28 + 4 heads, 33 us and 44 in two, 32 prompts over four of 2880
+    // 126 and 143.  With 32-bit rows it takes the registers of two blocks, which costs more than a launch where there are
+    // blocks enough: 16 answers over two prefixes of 3000, 64 + 8 heads (320 blocks), 50 and 69; those 64 answers (1264) 149 and 129.
+    p.both = p.own_kind != kWide && p.pre_kind != kWide && blocks_of(c, p.own) + blocks_of(c, p.pre) <= kMaxBlocks &&
+             (dtype == DART_BF16 || (c.d <= 128 && blocks_of(c, p.own) + blocks_of(c, p.pre) <= 1024));
+  }
+  if (p.parts > 1 && (long)c.T * c.Hq > kMaxJoined) return DART_ERR_SHAPE;
+  p.own.parts = p.pre.parts = p.parts;
+  auto up = [](size_t v) { return (v + kAlign - 1) / kAlign * kAlign; };
+  const size_t rows = (size_t)c.T * c.Hq;
+  p.total = kAlign;
+  if (p.parts > 1) {
+    p.o_ml = up((size_t)p.parts * rows * c.d * 4);
+    p.total = p.o_ml + up((size_t)p.parts * rows * 8);
+  }
+  return DART_OK;
+}
+
+// Lanes to a row, as powers of two, and how many sets of them share a row's parts.
+struct JoinPlan {
+  int lanes_shift, split_shift;
+  long blocks;
+};
+
+inline JoinPlan plan_join(const Cache& c, int parts) {
+  JoinPlan j = {};
+  while ((4 << j.lanes_shift) < c.d) ++j.lanes_shift;
+  // many parts of few rows are shared by up to a block's sets of lanes, four parts at least to each
+  while (j.split_shift < 8 - j.lanes_shift && (4 << j.split_shift) < parts && ((long)c.T * c.Hq << j.split_shift) < kJoinSets) ++j.split_shift;
+  const int rows_shift = 8 - j.lanes_shift - j.split_shift;
+  j.blocks = (((long)c.T * c.Hq - 1) >> rows_shift) + 1;
+  return j;
+}
+
+// Launches the join of a plan's parts (attend_api.hip).
+dart_status dart_attend_join(const Attend& a, const Cache& c, int dtype, const AttendPlan& p, hipStream_t st);
 
 }  // namespace dart

@@ -1,0 +1,35 @@
+// Attention over pages held in 4 bits.
+#pragma once
+
+#include "fourbit.hpp"
+#include "k_attend.hpp"
+
+namespace dart {
+
+// The tiles of attention over rows, keys and values brought to the rows' type on their way to LDS.
+template <int DT, int DP, int QW, int WM, int WK, int KT>
+__global__ __launch_bounds__(64 * WM * WK, DP <= 128 && (DT == kBF16 || WK == 1) ? 2 : 1) void k_attend_4bit(Attend a, Cache c, Parting sp) {
+  extern __shared__ __align__(16) unsigned char lds[];
+  __shared__ AttendShared sh;
+  long slot;
+  int head, part;
+  attend_place(c, sp, blockIdx.x, slot, head, part);
+  attend_tile<DT, DP, QW, WM, WK, KT, In4Bits>(a, c, sp, lds, sh, slot, head, part);
+}
+
+// Prefixes and own keys in one launch.
+template <int DT, int DP, int KT>
+__global__ __launch_bounds__(256, DT == kBF16 && DP <= 128 ? 2 : 1) void k_attend_4bit_both(Attend a, Cache c, Parting pre, Parting own,
+                                                                                            unsigned pre_blocks) {
+  extern __shared__ __align__(16) unsigned char lds[];
+  __shared__ AttendShared sh;
+  const bool first = blockIdx.x < pre_blocks;
+  const Parting sp = first ? pre : own;
+  long slot;
+  int head, part;
+  attend_place(c, sp, first ? blockIdx.x : blockIdx.x - pre_blocks, slot, head, part);
+  if (sp.few) attend_tile<DT, DP, 16, 1, 4, 32, In4Bits>(a, c, sp, lds, sh, slot, head, part);
+  else attend_tile<DT, DP, many_columns(DT, DP), 4, 1, KT, In4Bits>(a, c, sp, lds, sh, slot, head, part);
+}
+
+}  // namespace dart
