@@ -26,8 +26,11 @@ __device__ __forceinline__ void two_values(uint32_t codes, float scale, uint32_t
 }
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }  // (the conversions take its exponent)
 
+// A value that the compiler takes as new, so that what is made of it is made here and not kept over a loop.
+__device__ __forceinline__ void made_here(uint32_t& x) { asm volatile("" : "+v"(x)); }
+
 struct In4Bits {
-  static constexpr bool kCodes = true;
+  static constexpr bool kCodes = true, kPages = false;
   // Values of a load, where a thread has a share of them: 32 (a block), 16 or 8.
   static constexpr int unit(int, int share) { return share < kBlock ? share : kBlock; }
   __device__ static __forceinline__ bool no_number(uint32_t scale) { return scale == kNoNumber; }
@@ -68,6 +71,11 @@ struct In4Bits {
     }
     return p;
   }
+};
+
+// Pages of 16 rows and more, a row's stride small enough for 32 bits to hold 16 of them: tiles of 16 keys that lie in one page.
+struct In4BitsPages : In4Bits {
+  static constexpr bool kPages = true;
 };
 
 }  // namespace dart

@@ -39,14 +39,14 @@ void set_hold(Hold& a, const Cache& c) {
   a.per_block = a.blocks > 1 ? (uint32_t)(((1ull << 32) + a.blocks - 1) / a.blocks) : 0;
 }
 
-template <int DT, int DP, int QW, int WM, int WK, int KT>
+template <int DT, int DP, int QW, int WM, int WK, int KT, class HELD = In4Bits>
 dart_status launch_tiles(const Attend& a, const Cache& c, const Parting& sp, hipStream_t st) {
-  typedef AttendShape<DT, DP, QW, WM, WK, KT, In4Bits> S;
+  typedef AttendShape<DT, DP, QW, WM, WK, KT, HELD> S;
   const long most = kMaxBlocks / ((long)c.Hkv * sp.chunks);
   Parting left = sp;
   while (left.slots > 0) {
     const long slots = std::min(left.slots, most);
-    k_attend_4bit<DT, DP, QW, WM, WK, KT><<<dim3((unsigned)(slots * c.Hkv * sp.chunks)), dim3(S::kThreads), S::kLds, st>>>(a, c, left);
+    k_attend_4bit<DT, DP, QW, WM, WK, KT, HELD><<<dim3((unsigned)(slots * c.Hkv * sp.chunks)), dim3(S::kThreads), S::kLds, st>>>(a, c, left);
     DART_TRY(launched());
     left.slots -= slots;
   }
@@ -55,6 +55,8 @@ dart_status launch_tiles(const Attend& a, const Cache& c, const Parting& sp, hip
 
 template <int DT, int DP>
 dart_status launch_attend(const Attend& a, const Cache& c, const Parting& sp, Kind kind, hipStream_t st) {
+  if constexpr (DP <= 128)
+    if (kind == kFew && c.page_shift >= 4 && c.row_16 < 1u << 24) return launch_tiles<DT, DP, 16, 1, 4, 64, In4BitsPages>(a, c, sp, st);
   if constexpr (DT == kBF16 || DP <= 128)
     if (kind == kFew) return launch_tiles<DT, DP, 16, 1, 4, 32>(a, c, sp, st);
   if constexpr (DT == kBF16 && DP <= 128)
@@ -137,7 +139,7 @@ dart_status dart_read_4bit(const dart_cache* cache, const void* k_codes, const v
 size_t dart_attend_4bit_workspace_bytes(const dart_cache* cache) {
   Cache c;
   AttendPlan p;
-  if (make_cache(cache, c, 4) != DART_OK || plan_attend(c, cache->dtype, p) != DART_OK) return 0;
+  if (make_cache(cache, c, 4) != DART_OK || plan_attend(c, cache->dtype, p, true) != DART_OK) return 0;
   return p.total;
 }
 
@@ -153,7 +155,7 @@ dart_status dart_attend_4bit(const dart_cache* cache, const void* q, int64_t q_l
   DART_TRY(check_pool(k_codes, k_scales));
   DART_TRY(check_pool(v_codes, v_scales));
   AttendPlan p;
-  DART_TRY(plan_attend(c, cache->dtype, p));
+  DART_TRY(plan_attend(c, cache->dtype, p, true));
   if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < p.total) return DART_ERR_WORKSPACE;
   c.status = status;
   const Attend a = {q, k_codes, v_codes, out, lse, q_ld, out_ld, scale, causal != 0, 1.0 / (c.Hq / c.Hkv),

@@ -178,7 +178,7 @@ __device__ __forceinline__ int slot_owner(const Cache& c, const int* group_cu, i
 
 // Pools of rows of the queries' type: loads of 16 bytes.
 struct AsRows {
-  static constexpr bool kCodes = false;
+  static constexpr bool kCodes = false, kPages = false;
   static constexpr int unit(int piece, int) { return piece; }
 };
 
@@ -195,12 +195,18 @@ struct AttendShape {
   static constexpr int kLoads = KT * kPieces / kGroup;   // pieces of keys (and of values) per thread
   static constexpr int kApart = kGroup / kPieces;        // rows between a thread's pieces
   static constexpr int kBuffers = WM > 1 ? 2 : 1;
-  static constexpr int kTileBytes = KT * kRowBytes;
+  // Keys held as codes go from memory to the products of the one wave that takes them, without LDS.
+  static constexpr bool kDirect = HELD::kCodes && WM == 1;
+  // (pages of 16 rows and more: a step's values go to LDS 32 keys at a time)
+  static constexpr bool kPages = HELD::kPages;
+  static constexpr int kTileBytes = (kPages ? 32 : KT) * kRowBytes;
+  static constexpr int kBufferBytes = (kDirect ? 1 : 2) * kTileBytes;
   static constexpr int kBM = QW * WM;
-  static constexpr int kLds = WK * kBuffers * 2 * kTileBytes;
+  static constexpr int kLds = WK * kBuffers * kBufferBytes;
   static_assert(kGroup % kPieces == 0 && KT * kPieces % kGroup == 0 && KT % 32 == 0, "");
   static_assert(WK == 1 || WM == 1, "");
-  static_assert(WK == 1 || QW * DP * 4 <= kBuffers * 2 * kTileBytes, "joined in the tiles' place");
+  static_assert(!kPages || (kDirect && KT == 64 && QW == 16 && DP <= 128), "");
+  static_assert(WK == 1 || QW * DP * 4 <= kBuffers * kBufferBytes, "joined in the tiles' place");
 };
 
 // Columns of a wave's tile where four waves take the rows: 32 halve what LDS has to deliver per product, but with
@@ -301,16 +307,33 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   const unsigned char* vp = static_cast<const unsigned char*>(a.v_pool) + piece_at;
   const uint8_t* ks = HELD::kCodes ? a.k_scales + my_at / 32 : nullptr;
   const uint8_t* vs = HELD::kCodes ? a.v_scales + my_at / 32 : nullptr;
-  unsigned char* const my_lds = lds + wk * (S::kBuffers * 2 * S::kTileBytes);
+  unsigned char* const my_lds = lds + wk * (S::kBuffers * S::kBufferBytes);
   const int row_mask = (1 << c.page_shift) - 1, last_key = k1 - 1;
   typedef typename std::conditional<HELD::kCodes, Codes<S::kUnit / 8 ? S::kUnit / 8 : 1>, u32x4>::type Load;
   Load kr[S::kLoads], vr[S::kLoads];
   uint32_t ke[S::kLoads], ve[S::kLoads];  // (scales)
   int pg[S::kLoads];
   bool bad_page = false;
+  // (keys without LDS) of each of the step's keys in this lane's row of a tile, the DP / kGroups values of its group: blocks, or
+  // the half of one
+  constexpr int kMine = DP / M::kGroups, kDirectTiles = S::kDirect ? KT / QW : 1, kDirectLoads = kMine > 32 ? kMine / 32 : 1;
+  typedef Codes<(kMine < 32 ? kMine : 32) / 8> Direct;
+  Direct dk[kDirectTiles][kDirectLoads];
+  uint32_t de[kDirectTiles][kDirectLoads];
+  int dpg[kDirectTiles];
+  // (what lies past the head is the row's first block again, by queries of zeros)
+  const bool group_on = grp * kMine < c.d;
+  const long direct_at = (long)head * c.head_ld + (group_on ? grp * kMine : 0);
+  const unsigned char* dkp = static_cast<const unsigned char*>(a.k_pool) + direct_at / 2;
+  const uint8_t* dks = S::kDirect ? a.k_scales + direct_at / 32 : nullptr;
+  auto direct_on = [&](int j) { return group_on && grp * kMine + j * 32 < c.d; };
   auto load_pages = [&](int kb) {
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) pg[i] = table[min(kb + my_row + i * S::kApart, last_key) >> c.page_shift];
+    if constexpr (S::kDirect) {
+#pragma unroll
+      for (int t = 0; t < kDirectTiles; ++t) dpg[t] = table[min(kb + t * QW + col, last_key) >> c.page_shift];
+    }
   };
   // (page offsets by 32-bit products: the wider ones cost as much as a fifth of a step's exponentials)
   auto place_of = [&](int i, int kb) {
@@ -323,17 +346,31 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
       const uint64_t off = place_of(i, kb);
-      __builtin_memcpy(&kr[i], __builtin_assume_aligned(kp + (off << 4), sizeof(Load)), sizeof(Load));
+      if (!S::kDirect) __builtin_memcpy(&kr[i], __builtin_assume_aligned(kp + (off << 4), sizeof(Load)), sizeof(Load));
       __builtin_memcpy(&vr[i], __builtin_assume_aligned(vp + (off << 4), sizeof(Load)), sizeof(Load));
       if constexpr (HELD::kCodes) {
-        ke[i] = ks[off];
+        if (!S::kDirect) ke[i] = ks[off];
         ve[i] = vs[off];
+      }
+    }
+    if constexpr (S::kDirect) {
+#pragma unroll
+      for (int t = 0; t < kDirectTiles; ++t) {
+        int page = dpg[t];
+        if ((unsigned)page >= (unsigned)c.n_pages) page = 0, bad_page = true;
+        const uint32_t row = min(kb + t * QW + col, last_key) & row_mask;
+        const uint64_t off = (uint64_t)(uint32_t)page * c.page_16 + (uint64_t)row * c.row_16;
+#pragma unroll
+        for (int j = 0; j < kDirectLoads; ++j) {
+          __builtin_memcpy(&dk[t][j], __builtin_assume_aligned(dkp + (off << 4) + (direct_on(j) ? j * 16 : 0), sizeof(Direct)), sizeof(Direct));
+          de[t][j] = dks[off + (direct_on(j) ? j : 0)];
+        }
       }
     }
   };
   const int steps = (k1 - k0 + KT * WK - 1) / (KT * WK);
   const int kstep = KT * WK, kfirst = k0 + wk * KT;
-  if (steps > 0) load_pages(kfirst);
+  if (!S::kPages && steps > 0) load_pages(kfirst);
 
   // ---- this lane's query: the last key it sees, and its pieces
   const int my = row0 + wm * QW + col;
@@ -344,10 +381,12 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   const uint32_t flip = a.scale < 0.f ? (DT == kBF16 ? 0x80008000u : 0x80000000u) : 0u;  // (scores then scale by |scale|)
   const unsigned char* q_at =
       static_cast<const unsigned char*>(a.q) + ((long)(tok0 + my_tok) * a.q_ld + (long)qh * c.d) * S::kEsz;
+  // (a lane group's pieces of a row: every kGroups-th, or where keys come as codes one run of them)
+  auto piece_of = [&](int s) { return S::kDirect ? grp * kSteps + s : M::kGroups * s + grp; };
   u32x4 q[kSteps];
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
-    const int e = (M::kGroups * s + grp) * M::kVec;
+    const int e = piece_of(s) * M::kVec;
     u32x4 v = *reinterpret_cast<const u32x4*>(q_at + (e < c.d ? e : 0) * S::kEsz);
     // (scale 0: queries of zeros, so that a hidden score stays -infinity)
     v = e < c.d && a.scale != 0.f ? v ^ flip : u32x4{0, 0, 0, 0};
@@ -427,6 +466,22 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
 
   // ---- the three parts of a step: scores of its keys, 32 at a time in sc[sub]; their weights; the weighted values
   float sc[kSub][M::kScores];
+  Direct dk_now[kDirectTiles][kDirectLoads];
+  uint32_t de_now[kDirectTiles][kDirectLoads];
+  auto scores_direct = [&]() {
+    if constexpr (S::kDirect) {
+      constexpr int kPer = 32 / M::kVec;  // pieces of a block
+#pragma unroll
+      for (int t = 0; t < kDirectTiles; ++t) {
+        acc x = acc{};
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+          x = M::qk(HELD::template piece<DT>(dk_now[t][s / kPer].v[s % kPer * M::kVec / 8], de_now[t][s / kPer], s * M::kVec / 4 % 2), q[s], x);
+#pragma unroll
+        for (int i = 0; i < M::kRegs; ++i) sc[t / M::kTiles][t % M::kTiles * M::kRegs + i] = x[i];
+      }
+    }
+  };
   auto scores = [&](const unsigned char* kl) {
 #pragma unroll
     for (int t = 0; t < kSub * M::kTiles; ++t) {
@@ -519,10 +574,10 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     }
   };
   // (32-bit rows: a lane's 16 bytes feed four result tiles, whose rows are therefore every fourth element of the head)
-  auto values_f32 = [&](const unsigned char* vl, int sub) {
+  auto values_f32 = [&](const unsigned char* vl, int at, int sub) {  // (keys 32 * at on of the tile, weights of sub)
 #pragma unroll
     for (int u = 0; u < M::kScores; ++u) {
-      const int row = sub * 32 + M::place(u, grp);
+      const int row = at * 32 + M::place(u, grp);
 #pragma unroll
       for (int i = 0; i < kDT / 4; ++i) {
         const f32x4v v = *reinterpret_cast<const f32x4v*>(vl + row * RB + (((i * QW + col) ^ mix<RB>(row)) << 4));
@@ -533,6 +588,114 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     }
   };
 
+  if constexpr (S::kPages) {
+    // A tile of 16 keys lies in one page, so that its place is the same for all lanes but for what a lane adds within it, always
+    // the same.  A lane brings one of four runs of a key's values and of a value's; keys go to the products as they come, values
+    // by LDS.  The next step's keys are asked for when this one's scores are done, its values when the products are.
+    constexpr int kTiles = KT / QW, kSplit = kMine / M::kVec;
+    const int mine_at = grp * kMine;  // (the run of this lane among its key's; among its value's (lane & 3) * kMine)
+    const int v_row = (lane >> 4) + 4 * (lane >> 2 & 3), v_at = (lane & 3) * kMine;  // (so that eight lanes in a row meet no bank twice)
+    const uint32_t k_units = col * c.row_16 + (mine_at < c.d ? mine_at / 32 : 0), v_units = v_row * c.row_16 + (v_at < c.d ? v_at / 32 : 0);
+    const uint32_t k_bytes = (col * c.row_16 << 4) + (mine_at < c.d ? mine_at / 2 : 0);
+    const uint32_t v_bytes = (v_row * c.row_16 << 4) + (v_at < c.d ? v_at / 2 : 0);
+    const long head_units = (long)head * c.head_ld / 32;
+    Direct kc[kTiles], vc[kTiles];
+    uint32_t kx[kTiles], vx[kTiles];
+    const int mine = kfirst < k1 ? (k1 - 1 - kfirst) / kstep + 1 : 0;  // steps of this wave
+    // the pages of the wave's next 64 tiles, one to a lane
+    auto tile_key = [&](int n) { return min(kfirst + n / kTiles * kstep + n % kTiles * QW, last_key) & ~(QW - 1); };
+    auto pages_of = [&](int it) { return table[tile_key(it * kTiles + lane) >> c.page_shift]; };
+    int now = 0, next = 0;
+    long unit[kTiles];
+    auto places = [&](int it) {  // of a step's tiles, in units of 16 bytes of codes and of a scale
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        int page = __builtin_amdgcn_readlane(now, (it * kTiles + t) & 63);
+        if ((unsigned)page >= (unsigned)c.n_pages) page = 0, bad_page = true;
+        unit[t] = (long)((uint64_t)(uint32_t)page * c.page_16 + (uint64_t)(uint32_t)(tile_key(it * kTiles + t) & row_mask) * c.row_16) + head_units;
+      }
+    };
+    auto load_keys = [&]() {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        __builtin_memcpy(&kc[t], __builtin_assume_aligned(static_cast<const unsigned char*>(a.k_pool) + (unit[t] << 4) + k_bytes, sizeof(Direct)),
+                         sizeof(Direct));
+        kx[t] = (a.k_scales + unit[t])[k_units];
+      }
+    };
+    auto load_values = [&]() {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        __builtin_memcpy(&vc[t], __builtin_assume_aligned(static_cast<const unsigned char*>(a.v_pool) + (unit[t] << 4) + v_bytes, sizeof(Direct)),
+                         sizeof(Direct));
+        vx[t] = (a.v_scales + unit[t])[v_units];
+      }
+    };
+    if (mine > 0) {
+      now = pages_of(0);
+      next = mine > 16 ? pages_of(16) : 0;
+      places(0);
+      load_keys();
+      load_values();
+    }
+    for (int it = 0; it < mine; ++it) {
+      const int kb = kfirst + it * kstep;
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        acc x = acc{};
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+          x = M::qk(HELD::template piece<DT>(kc[t].v[s * M::kVec / 8], kx[t], s * M::kVec / 4 % 2), q[s], x);
+#pragma unroll
+        for (int i = 0; i < M::kRegs; ++i) sc[t / M::kTiles][t % M::kTiles * M::kRegs + i] = x[i];
+      }
+      const bool more = it + 1 < mine;
+      if (more) {
+        if ((it + 1) % 16 == 0) {
+          now = next;
+          next = it + 17 < mine ? pages_of(it + 17) : 0;
+        }
+        places(it + 1);
+        load_keys();
+      }
+      if (kb <= lim_last) reference(kb);
+      if (kb + KT > k1) {
+        // (what lies behind the keys may be anything; its weight is 0, and 0 times NaN is NaN)
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+          if (kb + t * QW + v_row >= k1) vc[t] = Direct{}, vx[t] = 0;
+      }
+      if (kb + KT - 1 > lim_block && causal) {
+        // (values that are no numbers and that some row does not see: left out here and added at the end)
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+          if (HELD::no_number(vx[t])) vc[t] = Direct{}, vx[t] = 0, sh.odd_values[wk] = 1;
+      }
+#pragma unroll
+      for (int sub = 0; sub < kSub; ++sub) {
+        tiles_handed_over();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = i * QW + v_row;
+#pragma unroll
+          for (int j = 0; j < kSplit; ++j)
+            *reinterpret_cast<u32x4*>(my_lds + row * RB + ((((lane & 3) * kSplit + j) ^ mix<RB>(row)) << 4)) =
+                HELD::template piece<DT>(vc[2 * sub + i].v[j * M::kVec / 8], vx[2 * sub + i], j * M::kVec / 4 % 2);
+        }
+        if (sub == kSub - 1 && more) load_values();
+        tiles_handed_over();
+        if (kb > lim_last) continue;
+        weights(sub);
+        if constexpr (DT == kBF16) {
+#pragma unroll
+          for (int s = 0; s < M::kScores / 8; ++s) values_bf16(my_lds, 0, s, packed(sub, s));
+        } else {
+          values_f32(my_lds, 0, sub);
+        }
+      }
+    }
+    __syncthreads();  // (the tiles' place is the results' now)
+  } else {
   if (steps > 0) {
     load_tile(kfirst);
     load_pages(kfirst + kstep);
@@ -540,17 +703,25 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   __syncthreads();
   for (int it = 0; it < steps; ++it) {
     const int kb = kfirst + it * kstep;
-    unsigned char* kl = my_lds + (S::kBuffers > 1 ? (it & 1) * 2 * S::kTileBytes : 0);
-    unsigned char* vl = kl + S::kTileBytes;
+    unsigned char* kl = my_lds + (S::kBuffers > 1 ? (it & 1) * S::kBufferBytes : 0);
+    unsigned char* vl = S::kDirect ? kl : kl + S::kTileBytes;
     if (S::kBuffers == 1) tiles_handed_over();
-    store_keys(kl);
+    if constexpr (S::kDirect) {
+#pragma unroll
+      for (int t = 0; t < kDirectTiles; ++t)
+#pragma unroll
+        for (int j = 0; j < kDirectLoads; ++j) dk_now[t][j] = dk[t][j], de_now[t][j] = de[t][j];
+    } else {
+      store_keys(kl);
+    }
     store_values(vl, kb);
     load_tile(kb + kstep);
     load_pages(kb + 2 * kstep);
     if (WM > 1) __syncthreads();
     else tiles_handed_over();
     if (kb > lim_last) continue;  // (none of this wave's rows sees a key of the step)
-    scores(kl);
+    if constexpr (S::kDirect) scores_direct();
+    else scores(kl);
     reference(kb);
 #pragma unroll
     for (int sub = 0; sub < kSub; ++sub) {
@@ -559,9 +730,10 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
 #pragma unroll
         for (int s = 0; s < M::kScores / 8; ++s) values_bf16(vl, sub, s, packed(sub, s));
       } else {
-        values_f32(vl, sub);
+        values_f32(vl, sub, sub);
       }
     }
+  }
   }
   if (bad_page) flag(c, kBadPage);
   if (causal) {
@@ -577,7 +749,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
         float w = 0.f;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-          const int e = (M::kGroups * s + grp) * M::kVec;
+          const int e = piece_of(s) * M::kVec;
           Piece<DT, M::kVec> kf = {}, qf;
           if (e < c.d) {
             if constexpr (HELD::kCodes) kf = HELD::template values<DT, M::kVec>(a.k_pool, a.k_scales, at + e);
@@ -653,7 +825,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
       f32x4v x = {};
 #pragma unroll
       for (int w = 0; w < WK; ++w)
-        x += *reinterpret_cast<const f32x4v*>(reinterpret_cast<const float*>(lds + w * (S::kBuffers * 2 * S::kTileBytes)) + rr * DP +
+        x += *reinterpret_cast<const f32x4v*>(reinterpret_cast<const float*>(lds + w * (S::kBuffers * S::kBufferBytes)) + rr * DP +
                                               ((piece ^ (rr & 7)) << 2));
       const int i = token_in(a, row), h = head * r + row - i * r;
       const long id = (long)(tok0 + i) * c.Hq + h;
@@ -851,7 +1023,8 @@ inline long blocks_of(const Cache& c, const Parting& p) { return p.slots * c.Hkv
 // over four prefixes of 2880 53 us with 16 sequences to each, 65 with 61, 1, 1 and 1.  max_keys: the caller's bound, which
 // divides the keys, whatever the lengths are: one token over 2000 keys, 28 + 4 heads, 12.4 us, 27 with a bound of 131 072; 32 of
 // them 28 and 44.
-inline Kind plan_parting(const Cache& c, int dtype, bool prefix, long rows, int owners, int max_keys, Parting& p) {
+inline Kind plan_parting(const Cache& c, int dtype, bool prefix, long rows, int owners, int max_keys, Parting& p,
+                         bool codes = false) {
   const int r = c.Hq / c.Hkv;
   // 256-row tiles take the least from LDS and caches per row, but each has a compute unit to itself, so that nothing
   // hides its start and end: they pay from 1024 keys and 1.5 tiles to a unit on.  28 + 4 heads, causal, 128- and
@@ -879,22 +1052,24 @@ inline Kind plan_parting(const Cache& c, int dtype, bool prefix, long rows, int 
   // join: 64 rows of 28 + 4 heads over 8000 keys 197 us in one part, 40 in 128 blocks, 31 in 256, 33 in 512, 46 in
   // 1024; 64 answers over one prefix of 9216 229, 43, 34, 42 and 48.  32-bit tiles of four waves are bound by the
   // matrix cores' latency and want company: 637 causal tokens of 32 heads 69 us in 320 blocks, 58 in 960.
-  const long want = std::max(1L, (dtype == DART_F32 && kind == kMany ? 1024 : 256) / blocks);
+  // Keys held in 4 bits are a quarter of the bytes, and single tokens need two blocks to a unit to have them come as fast: 32 tokens over
+  // 8704 keys each, 28 + 4 heads, 45 us with 256 blocks, 36 with 512, 42 with 1024; 64 over 4352 41, 35 and 43.
+  const long want = std::max(1L, (dtype == DART_F32 && kind == kMany ? 1024 : codes && kind == kFew ? 512 : 256) / blocks);
   const long chunk = std::max(256L, ((max_keys + want - 1) / want + 255) / 256 * 256);
   p.chunk = (int)chunk;
   p.chunks = std::max(1, (int)((max_keys + chunk - 1) / chunk));
   return kind;
 }
 
-inline dart_status plan_attend(const Cache& c, int dtype, AttendPlan& p) {
+inline dart_status plan_attend(const Cache& c, int dtype, AttendPlan& p, bool codes = false) {
   const int r = c.Hq / c.Hkv;
   if ((long)c.T * r > kMaxRows) return DART_ERR_SHAPE;
   p = {};
-  p.own_kind = plan_parting(c, dtype, false, (long)c.max_q * r, c.B, c.max_kv, p.own);
+  p.own_kind = plan_parting(c, dtype, false, (long)c.max_q * r, c.B, c.max_kv, p.own, codes);
   p.parts = p.own.chunks;
   if (c.groups > 0) {
     const long rows = std::min((long)c.T, (long)c.max_q * c.B) * r;
-    p.pre_kind = plan_parting(c, dtype, true, std::max(1L, (rows + c.groups - 1) / c.groups), c.groups, c.max_prefix, p.pre);
+    p.pre_kind = plan_parting(c, dtype, true, std::max(1L, (rows + c.groups - 1) / c.groups), c.groups, c.max_prefix, p.pre, codes);
     p.parts += p.pre.chunks;
     p.own.first_part = p.pre.chunks;
     // One launch for both: 64 answers over a prefix of 9216 keys, 28 + 4 heads, 33 us and 44 in two, 32 prompts over four of 2880

@@ -7,14 +7,14 @@
 namespace dart {
 
 // The tiles of attention over rows, keys and values brought to the rows' type on their way to LDS.
-template <int DT, int DP, int QW, int WM, int WK, int KT>
-__global__ __launch_bounds__(64 * WM * WK, DP <= 128 && (DT == kBF16 || WK == 1) ? 2 : 1) void k_attend_4bit(Attend a, Cache c, Parting sp) {
+template <int DT, int DP, int QW, int WM, int WK, int KT, class HELD>
+__global__ __launch_bounds__(64 * WM * WK, HELD::kPages && DT == kBF16 ? 3 : DP <= 128 && (DT == kBF16 || WK == 1) ? 2 : 1) void k_attend_4bit(Attend a, Cache c, Parting sp) {
   extern __shared__ __align__(16) unsigned char lds[];
   __shared__ AttendShared sh;
   long slot;
   int head, part;
   attend_place(c, sp, blockIdx.x, slot, head, part);
-  attend_tile<DT, DP, QW, WM, WK, KT, In4Bits>(a, c, sp, lds, sh, slot, head, part);
+  attend_tile<DT, DP, QW, WM, WK, KT, HELD>(a, c, sp, lds, sh, slot, head, part);
 }
 
 // Prefixes and own keys in one launch.

@@ -5,6 +5,7 @@
 
 struct int2 { int x, y; };
 inline int2 make_int2(int x, int y) { return {x, y}; }
+inline uint2 make_uint2(unsigned x, unsigned y) { return {x, y}; }
 
 extern dim3 lanes_grid, lanes_block;
 inline void lanes_shape(dim3 grid, dim3 block, size_t, hipStream_t) { lanes_grid = grid, lanes_block = block; }

@@ -33,6 +33,7 @@ def sources():
         files[name + ".cpp"] = L.replaced(api, '"../../include/dart.h"', '"dart.h"', 1)
     for name in ("fourbit.hpp", "k_fourbit.hpp", "k_attend4.hpp", "k_weights.hpp", "k_evict.hpp"):
         text = read(name).replace("extern __shared__ __align__(16) unsigned char lds[];", "unsigned char* const lds = lanes_lds();")
+        text = text.replace('asm volatile("" : "+v"(x));', "")  # (which only holds the compiler)
         files[name] = text.replace("(__attribute__((address_space(3))) ", "(")
     # (a wave's loads have come back: on the CPU they always have)
     files["common.hpp"] = L.replaced(files["common.hpp"], 'asm volatile("s_waitcnt vmcnt(0)" ::: "memory");', "", 1)
