@@ -30,24 +30,40 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return w != w ? 0u : u >> 31 ? ~u : u | 0x80000000u;
 }
 
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave;
-constexpr int kSelectHeld = 16;  // keys of a thread that it holds
-constexpr int kBuckets = 2048;
+constexpr int kBuckets = 2048, kListed = 128;
 
+// What a block of W waves keeps in LDS.
+template <int W>
 struct SelectShared {
   int bucket[kBuckets];
-  uint32_t low[kSelectWaves], high[kSelectWaves];
-  int wave_sum[kSelectWaves];
-  int found, before, inside, bad;
-  int above[kSelectHeld * kSelectWaves], equal[kSelectHeld * kSelectWaves];
+  uint32_t low[W], high[W];
+  int wave_sum[W];
+  int found, before, inside, bad, listed, last;
+  uint32_t border;
+  unsigned long long list[kListed];  // weights about the border, and below them places from the last on
 };
 
+// Over the lanes up to this one.
+__device__ __forceinline__ int lanes_sum(int x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
 // Chooses the keys of one key head of one sequence: `first` and `recent` ones, and of those between the ones of largest weight,
-// of equals the first.  The border is found from the top: the range of the weights that are left, as whole numbers of their
-// order, is cut in 2048 buckets, and the one that the border falls in is the next range.  Then the keys are counted up to their
-// places in order.  A block of 16 waves; up to 16 384 keys are read once and held in registers.
-__global__ __launch_bounds__(kSelectThreads) void k_evict_select(Evict a, Cache c) {
-  __shared__ SelectShared sh;
+// of equals the first.  The border is the last key taken, by (weight, place).  It is found from the top: the range of the weights that
+// are left, as whole numbers of their order, is cut in 2048 buckets, and the one that the border falls in is the next range,
+// until so few weights are left that each is compared with all others, or all that are left are alike.  Then the keys up to the
+// border are counted to their places in order.  A block of W waves, a wave H times 64 keys in a row; so many keys (H * W * 64)
+// are read once and held in registers, longer sequences are read again by every step.
+template <int W, int H>
+__global__ __launch_bounds__(W * kWave) void k_evict_select(Evict a, Cache c) {
+  __shared__ SelectShared<W> sh;
+  constexpr int kThreads = W * kWave, kHeld = kThreads * H;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const long pairs = (long)c.B * c.Hkv;
   for (long id = blockIdx.x; id < pairs; id += gridDim.x) {
@@ -62,134 +78,181 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(Evict a, Cache 
     if (!valid) continue;
     int* kept = a.kept + id * a.kept_ld;
     if (keep == kv) {
-      for (int j = tid; j < kv; j += kSelectThreads) kept[j] = j;
+      for (int j = tid; j < kv; j += kThreads) kept[j] = j;
       continue;
     }
     const int* table = c.pages + (long)b * c.pages_ld;
     // candidates first .. first + n - 1, of which `want` are taken
     const int n = kv - a.recent - a.first, want = keep - a.recent - a.first;
-    for (int j = tid; j < a.first; j += kSelectThreads) kept[j] = j;
-    for (int j = tid; j < a.recent; j += kSelectThreads) kept[a.first + want + j] = kv - a.recent + j;
-    const int groups = (n + kSelectHeld * kSelectThreads - 1) / (kSelectHeld * kSelectThreads);
-    uint32_t u[kSelectHeld];
+    for (int j = tid; j < a.first; j += kThreads) kept[j] = j;
+    for (int j = tid; j < a.recent; j += kThreads) kept[a.first + want + j] = kv - a.recent + j;
+    const int groups = (n + kHeld - 1) / kHeld;
+    uint32_t u[H];
     bool bad = false;
+    auto place = [&](int g, int i) { return g * kHeld + (wave * H + i) * kWave + lane; };
     auto load = [&](int g) {
-      int page[kSelectHeld];
+      int page[H];
 #pragma unroll
-      for (int i = 0; i < kSelectHeld; ++i) {
-        const int x = (g * kSelectHeld + i) * kSelectThreads + tid;
-        page[i] = table[(a.first + (x < n ? x : n - 1)) >> c.page_shift];
-      }
+      for (int i = 0; i < H; ++i) page[i] = table[(a.first + min(place(g, i), n - 1)) >> c.page_shift];
 #pragma unroll
-      for (int i = 0; i < kSelectHeld; ++i) {
-        const int x = (g * kSelectHeld + i) * kSelectThreads + tid;
+      for (int i = 0; i < H; ++i) {
         const bool none = (unsigned)page[i] >= (unsigned)c.n_pages;
-        const int row = (a.first + (x < n ? x : n - 1)) & ((1 << c.page_shift) - 1);
+        const int row = (a.first + min(place(g, i), n - 1)) & ((1 << c.page_shift) - 1);
         const float w = a.weights[(((long)(none ? 0 : page[i]) * c.Hkv + h) << c.page_shift) + row];
         u[i] = none ? 0u : order_of(w);
         bad = bad || none;
       }
     };
-    auto counts = [&](int g, int i) { return (g * kSelectHeld + i) * kSelectThreads + tid < n; };
 
-    // ---- the range of the weights
+    // ---- the range of the weights (past the last the last again)
     uint32_t lo = 0xffffffffu, hi = 0;
     for (int g = 0; g < groups; ++g) {
       load(g);
 #pragma unroll
-      for (int i = 0; i < kSelectHeld; ++i)
-        if (counts(g, i)) lo = u[i] < lo ? u[i] : lo, hi = u[i] > hi ? u[i] : hi;
+      for (int i = 0; i < H; ++i) lo = u[i] < lo ? u[i] : lo, hi = u[i] > hi ? u[i] : hi;
     }
+    for (int x = tid; x < kBuckets; x += kThreads) sh.bucket[x] = 0;
+#pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
       const uint32_t l = __shfl_xor(lo, o), m = __shfl_xor(hi, o);
       lo = l < lo ? l : lo, hi = m > hi ? m : hi;
     }
-    __syncthreads();  // (of the block's work before)
     if (lane == 0) sh.low[wave] = lo, sh.high[wave] = hi;
-    if (tid == 0) sh.bad = 0;
+    if (tid == 0) sh.bad = 0, sh.listed = 0;
     __syncthreads();
-    for (int w = 0; w < kSelectWaves; ++w) {
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
       lo = sh.low[w] < lo ? sh.low[w] : lo;
       hi = sh.high[w] > hi ? sh.high[w] : hi;
     }
     if (bad) sh.bad = 1;
 
     // ---- the border: [lo, lo + 2^bits) holds it; `need` of the weights in it are taken, all above are
-    int bits = hi == lo ? 0 : 32 - __builtin_clz(hi - lo), need = want;
-    while (bits > 0 && need > 0) {
+    int bits = hi == lo ? 0 : 32 - __builtin_clz(hi - lo), need = want, inside = n;
+    while (bits > 0 && need > 0 && inside > kListed) {
       const int shift = bits > 11 ? bits - 11 : 0;
       const uint32_t used = 1u << (bits - shift);  // buckets
-      for (int x = tid; x < kBuckets; x += kSelectThreads) sh.bucket[x] = 0;
-      __syncthreads();
       for (int g = 0; g < groups; ++g) {
         if (groups > 1) load(g);
 #pragma unroll
-        for (int i = 0; i < kSelectHeld; ++i) {
-          const uint32_t x = (u[i] - lo) >> shift;
-          if (counts(g, i) && u[i] >= lo && x < used) atomicAdd(&sh.bucket[x], 1);
+        for (int i = 0; i < H; ++i) {
+          const uint32_t x = (u[i] - lo) >> shift;  // (weights below lo are far above)
+          if (place(g, i) < n && x < used) atomicAdd(&sh.bucket[x], 1);
         }
       }
       __syncthreads();
-      // weights in buckets above one's own two, from the sums of the waves above and of the lanes above
-      const int top = kBuckets - 1 - 2 * tid, c0 = sh.bucket[top], c1 = sh.bucket[top - 1];
-      int upto = c0 + c1;
-      for (int o = 1; o < kWave; o <<= 1) {
-        const int y = __shfl_up(upto, o);
-        if (lane >= o) upto += y;
-      }
+      // a thread's run of buckets, from the top; weights above it, from the sums of the lanes and the waves above
+      constexpr int kRun = kBuckets / kThreads;
+      int mine[kRun], all = 0;
+      const int top = kBuckets - 1 - kRun * tid;
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) mine[i] = sh.bucket[top - i], all += mine[i], sh.bucket[top - i] = 0;
+      const int upto = lanes_sum(all);
       if (lane == kWave - 1) sh.wave_sum[wave] = upto;
       __syncthreads();
-      int over = upto - c0 - c1;
-      for (int w = 0; w < wave; ++w) over += sh.wave_sum[w];
-      if (over < need && need <= over + c0) sh.found = top, sh.before = over, sh.inside = c0;
-      else if (over + c0 < need && need <= over + c0 + c1) sh.found = top - 1, sh.before = over + c0, sh.inside = c1;
+      int over = upto - all;
+#pragma unroll
+      for (int w = 0; w < W; ++w) over += w < wave ? sh.wave_sum[w] : 0;
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) {
+        if (over < need && need <= over + mine[i]) sh.found = top - i, sh.before = over, sh.inside = mine[i];
+        over += mine[i];
+      }
       __syncthreads();
       lo += (uint32_t)sh.found << shift;
       need -= sh.before;
+      inside = sh.inside;
       bits = shift;
-      const bool all = need == sh.inside;
-      __syncthreads();
-      if (all) break;
     }
     const uint32_t span = bits >= 32 ? 0xffffffffu : (1u << bits) - 1u;
-    // (nothing wanted: the border lies above all; a range that ends at the top of the order has nothing above it)
-    auto is_above = [&](uint32_t x) { return want > 0 && x > lo && x - lo > span; };
-    auto is_equal = [&](uint32_t x) { return want > 0 && x >= lo && x - lo <= span; };
+    if (tid == 0) sh.border = 0xffffffffu, sh.last = -1;  // (nothing wanted)
+    if (need > 0 && inside <= kListed) {
+      for (int g = 0; g < groups; ++g) {
+        if (groups > 1) load(g);
+        uint32_t in = 0;
+        int all = 0, at = 0;
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+          const bool x = place(g, i) < n && u[i] - lo <= span;
+          in |= (x ? 1u : 0u) << i;
+          all += __popcll(__ballot(x));
+        }
+        if (lane == 0 && all > 0) at = atomicAdd(&sh.listed, all);  // (in any order)
+        at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+          const unsigned long long m = __ballot(in >> i & 1);
+          if (in >> i & 1) sh.list[at + __popcll(m & ((1ull << lane) - 1ull))] = (unsigned long long)u[i] << 32 | ~(uint32_t)place(g, i);
+          at += __popcll(m);
+        }
+      }
+      __syncthreads();
+      // a wave compares its entries with all of them, which its lanes hold
+      constexpr int kPer = kListed / kWave;
+      unsigned long long all[kPer];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) all[i] = i * kWave + lane < inside ? sh.list[i * kWave + lane] : 0ull;
+      for (int x = wave; x < inside; x += W) {
+        const unsigned long long mine = sh.list[x];
+        int before = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) before += __popcll(__ballot(all[i] > mine));
+        if (before == need - 1 && lane == 0) sh.border = (uint32_t)(mine >> 32), sh.last = (int)~(uint32_t)mine;
+      }
+    } else if (need > 0) {  // all alike: the need-th of them in order
+      int done = 0;
+      for (int g = 0; g < groups; ++g) {
+        if (groups > 1) load(g);
+        int all = 0;
+#pragma unroll
+        for (int i = 0; i < H; ++i) all += __popcll(__ballot(place(g, i) < n && u[i] == lo));
+        if (lane == 0) sh.wave_sum[wave] = all;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < W; ++w) done += w < wave ? sh.wave_sum[w] : 0;
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+          const bool same = place(g, i) < n && u[i] == lo;
+          const unsigned long long e = __ballot(same);
+          if (same && done + __popcll(e & ((1ull << lane) - 1ull)) == need - 1) sh.border = lo, sh.last = place(g, i);
+          done += __popcll(e);
+        }
+#pragma unroll
+        for (int w = 0; w < W; ++w) done += w > wave ? sh.wave_sum[w] : 0;
+        __syncthreads();
+      }
+    }
+    __syncthreads();
+    const uint32_t border = sh.border;
+    const int last = sh.last;
 
-    // ---- places: of the keys above the border and of those at it, counted by wave and round
-    int done_above = 0, done_equal = 0;
+    // ---- places, by wave, round and lane
+    int done = 0;
     for (int g = 0; g < groups; ++g) {
       if (groups > 1) load(g);
+      uint32_t taken = 0;
+      int all = 0;
 #pragma unroll
-      for (int i = 0; i < kSelectHeld; ++i) {
-        const unsigned long long m = __ballot(counts(g, i) && is_above(u[i])), e = __ballot(counts(g, i) && is_equal(u[i]));
-        if (lane == 0) sh.above[i * kSelectWaves + wave] = __popcll(m), sh.equal[i * kSelectWaves + wave] = __popcll(e);
+      for (int i = 0; i < H; ++i) {
+        const bool t = place(g, i) < n && (u[i] > border || (u[i] == border && place(g, i) <= last));
+        taken |= (t ? 1u : 0u) << i;
+        all += __popcll(__ballot(t));
       }
+      if (lane == 0) sh.wave_sum[wave] = all;
       __syncthreads();
-      if (tid < kSelectHeld * kSelectWaves) {
-        int m = sh.above[tid], e = sh.equal[tid];
-        const int m0 = m, e0 = e;
-        for (int o = 1; o < kWave; o <<= 1) {
-          const int x = __shfl_up(m, o), y = __shfl_up(e, o);
-          if (lane >= o) m += x, e += y;
-        }
-        if (lane == kWave - 1) sh.wave_sum[wave] = m, sh.wave_sum[kSelectHeld * kSelectWaves / kWave + wave] = e;
-        sh.above[tid] = m - m0, sh.equal[tid] = e - e0;
-      }
-      __syncthreads();
-      constexpr int kFour = kSelectHeld * kSelectWaves / kWave;
+      int to = done;
 #pragma unroll
-      for (int i = 0; i < kSelectHeld; ++i) {
-        const bool m = counts(g, i) && is_above(u[i]), e = counts(g, i) && is_equal(u[i]);
-        const unsigned long long mm = __ballot(m), ee = __ballot(e), mine = (1ull << lane) - 1ull;
-        const int place = i * kSelectWaves + wave;
-        int na = done_above + sh.above[place] + __popcll(mm & mine), ne = done_equal + sh.equal[place] + __popcll(ee & mine);
-        for (int w = 0; w < place / kWave; ++w) na += sh.wave_sum[w], ne += sh.wave_sum[kFour + w];
-        // (the keys at the border before this one that are taken: `need` of them at most)
-        const int x = (g * kSelectHeld + i) * kSelectThreads + tid;
-        if (m || (e && ne < need)) kept[a.first + na + (ne < need ? ne : need)] = a.first + x;
+      for (int w = 0; w < W; ++w) {
+        const int x = sh.wave_sum[w];
+        done += x;
+        to += w < wave ? x : 0;
       }
-      for (int w = 0; w < kFour; ++w) done_above += sh.wave_sum[w], done_equal += sh.wave_sum[kFour + w];
+#pragma unroll
+      for (int i = 0; i < H; ++i) {
+        const unsigned long long m = __ballot(taken >> i & 1);
+        if (taken >> i & 1) kept[a.first + to + __popcll(m & ((1ull << lane) - 1ull))] = a.first + place(g, i);
+        to += __popcll(m);
+      }
       __syncthreads();
     }
     if (tid == 0 && sh.bad) flag(c, kBadPage);

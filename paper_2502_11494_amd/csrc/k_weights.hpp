@@ -21,20 +21,22 @@ struct Gather {
 struct Shares {
   int prefix;  // the keys are the groups' shared prefixes (else each sequence's own)
   int tiles;   // of keys, of the longest
+  int few;     // the kernel for few rows
   int parts;   // of the rows
   float* sums; // [parts][blocks of a part][keys of a tile], where there is more than one part
 };
 
-// 32 keys by 32 queries: keys in the rows of the product, queries in its columns.
+// 32 rows by 32 keys: a lane holds of its key the products with rows 8 (u / 4) + 4 (lane / 32) + u % 4, so that what a key
+// gathers is added up within the lane.
 template <int DT>
 struct Tile32 {
   static constexpr int kVec = DT == kBF16 ? 8 : 4;
-  __device__ static __forceinline__ f32x16 product(const u32x4& k, const u32x4& q, f32x16 c) {
+  __device__ static __forceinline__ f32x16 product(const u32x4& q, const u32x4& k, f32x16 c) {
     if constexpr (DT == kBF16) {
-      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, q), __builtin_bit_cast(bf16x8, k), c, 0, 0, 0);
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[j]), __uint_as_float(q[j]), c, 0, 0, 0);
+      for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(q[j]), __uint_as_float(k[j]), c, 0, 0, 0);
       return c;
     }
   }
@@ -47,9 +49,10 @@ struct GatherShape {
   static constexpr int kKeys = 128 * KW;
   static constexpr int kRowBytes = DP * (DT == kBF16 ? 2 : 4);
   static constexpr int kPieces = kRowBytes / 16;
-  static constexpr int kLoads = 32 * kPieces / 256 > 0 ? 32 * kPieces / 256 : 1;
-  static constexpr int kTile = 32 * kRowBytes;
-  static constexpr int kLds = 2 * kTile;
+  static constexpr int kRows = kRowBytes <= 512 ? 64 : 32;  // of a stage: what the block brings to LDS between two barriers
+  static constexpr int kLoads = kRows * kPieces / 256;
+  static constexpr int kStage = kRows * kRowBytes;
+  static constexpr int kLds = 2 * kStage;
 };
 
 // Whose rows and keys a block has.  n < 0: there is nothing to do for it.
@@ -98,7 +101,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_gather_weights(Gathe
   typedef Tile32<DT> M;
   constexpr int KW = S::KW, RB = S::kRowBytes, kSteps = DP / (2 * M::kVec);
   extern __shared__ __align__(16) unsigned char lds[];
-  __shared__ float2 row_of[2][32];  // a row's lse times log2 e, and the last key that it sees
+  __shared__ long row_at[2][64];
+  __shared__ f32x4v less_of[3][16];  // four rows' lse times log2 e
+  __shared__ int lim_of[3][64];      // the last key that a row sees
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, grp = lane >> 5, col = lane & 31;
   const int r = c.Hq / c.Hkv;
 
@@ -114,10 +119,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_gather_weights(Gathe
   if (!s.valid || s.n <= 0 || k0 >= s.kv) return;
   const bool causal = a.causal && !sp.prefix;
   const int rows = s.n * r;
-  // the rows from the first on that sees the first key of the tile, 32 at a time, dealt to the parts
-  const int row_first = causal ? max(0, k0 - s.fresh) * r : 0;
-  const int all = (rows - row_first + 31) / 32;
-  const int t0 = (int)((long)all * part / sp.parts), t1 = (int)((long)all * (part + 1) / sp.parts);
+  // Stages of rows, dealt to the parts alike for all tiles (so that tiles that are worked on side by side read the same rows, which
+  // then come from the die's cache), from the first on that has a row that sees the first key of the tile.
+  const int stages = (rows + S::kRows - 1) / S::kRows, seen_from = causal ? max(0, k0 - s.fresh) * r / S::kRows : 0;
+  const int t0 = max(seen_from, (int)((long)stages * part / sp.parts)), t1 = (int)((long)stages * (part + 1) / sp.parts);
 
   // ---- this lane's keys: of key `col` of 32 the pieces piece(s)
   auto piece = [&](int st) { return HELD::kCodes ? grp * kSteps + st : 2 * st + grp; };
@@ -154,102 +159,128 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_gather_weights(Gathe
     }
   }
 
-  // ---- rows to LDS
+  // ---- rows to LDS.  Where the rows of a stage lie is found three stages before, by a thread each (by all threads for themselves it
+  // costs as much as a third of the exponentials).
   const int my_piece = threadIdx.x % S::kPieces, my_row = threadIdx.x / S::kPieces;
   constexpr int kApart = 256 / S::kPieces;
+  const bool in_head = my_piece * M::kVec < c.d && a.scale != 0.f;  // (else zeros, from the start on)
+  const unsigned char* q_at = static_cast<const unsigned char*>(a.q) + ((long)s.tok0 * a.q_ld + (long)head * r * c.d + (in_head ? my_piece * M::kVec : 0)) * (16 / M::kVec);
+  const float* lse_at = a.lse + (long)s.tok0 * c.Hq + head * r;
+  const bool finds = (int)threadIdx.x < S::kRows;
+  float lse = 0.f;
+  int tok = 0, lim = 0;
+  long at = 0;
+  auto find_rows = [&](int t) {
+    if (!finds) return;
+    const int row = t * S::kRows + (int)threadIdx.x, have = min(row, rows - 1);  // (past the last: the last again)
+    tok = (int)(((double)have + 0.5) * a.per_token);
+    const int h = have - tok * r;
+    lse = lse_at[(long)tok * c.Hq + h];
+    lim = row >= rows ? -1 : causal ? min(s.fresh + tok, last_key) : last_key;
+    at = ((long)tok * a.q_ld + (long)h * c.d) * (16 / M::kVec);
+  };
+  auto tell_rows = [&](int t) {
+    if (!finds) return;
+    // (a row past the last, or one that saw nothing, gives nothing to any key)
+    row_at[t & 1][threadIdx.x] = at;
+    reinterpret_cast<float*>(less_of[t % 3])[threadIdx.x] = lse * kLog2e;
+    lim_of[t % 3][threadIdx.x] = lse == -INFINITY ? -1 : lim;
+  };
   u32x4 qr[S::kLoads];
-  float2 mine;
   auto load_rows = [&](int t) {
-    const int row0 = row_first + t * 32;
 #pragma unroll
-    for (int i = 0; i < S::kLoads; ++i) {
-      const int row = min(row0 + my_row + i * kApart, rows - 1), tok = (int)(((double)row + 0.5) * a.per_token);
-      const long at = (long)(s.tok0 + tok) * a.q_ld + (long)(head * r + row - tok * r) * c.d + my_piece * M::kVec;
-      qr[i] = u32x4{0, 0, 0, 0};
-      if (my_piece * M::kVec < c.d && a.scale != 0.f && my_row < 32)
-        qr[i] = *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(a.q) + at * (16 / M::kVec));
-    }
-    if (threadIdx.x < 32) {
-      const int row = row0 + (int)threadIdx.x, have = min(row, rows - 1), tok = (int)(((double)have + 0.5) * a.per_token);
-      const float lse = a.lse[(long)(s.tok0 + tok) * c.Hq + head * r + have - tok * r];
-      // (a row past the last, or one that saw nothing, gives nothing to any key)
-      const int lim = row >= rows || lse == -INFINITY ? -1 : causal ? min(s.fresh + tok, last_key) : last_key;
-      mine = make_float2(lse * kLog2e, __int_as_float(lim));
-    }
+    for (int i = 0; i < S::kLoads; ++i) qr[i] = *reinterpret_cast<const u32x4*>(q_at + row_at[t & 1][my_row + i * kApart]);
   };
   auto store_rows = [&](int t) {
-    unsigned char* to = lds + (t & 1) * S::kTile;
+    unsigned char* to = lds + (t & 1) * S::kStage;
+    if (!in_head) return;
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
       const int row = my_row + i * kApart;
-      if (row < 32) *reinterpret_cast<u32x4*>(to + row * RB + ((my_piece ^ mix<RB>(row)) << 4)) = qr[i];
+      *reinterpret_cast<u32x4*>(to + row * RB + ((my_piece ^ mix<RB>(row)) << 4)) = qr[i];
     }
-    if (threadIdx.x < 32) row_of[t & 1][threadIdx.x] = mine;
   };
-
-  const float scale2 = a.scale * kLog2e;
-  const int my_k0 = k0 + wave * KW * 32, my_end = my_k0 + KW * 32 - 1;
-  f32x16 sum[KW], total[KW];
+  if (!in_head) {
 #pragma unroll
-  for (int w = 0; w < KW; ++w) sum[w] = total[w] = f32x16{};
-  if (t0 < t1) load_rows(t0);
-  for (int t = t0; t < t1; ++t) {
-    store_rows(t);
-    __syncthreads();
-    if (t + 1 < t1) load_rows(t + 1);
-    const unsigned char* from = lds + (t & 1) * S::kTile;
-    f32x16 x[KW];
-#pragma unroll
-    for (int w = 0; w < KW; ++w) x[w] = f32x16{};
-#pragma unroll
-    for (int st = 0; st < kSteps; ++st) {
-      const u32x4 q = *reinterpret_cast<const u32x4*>(from + col * RB + ((piece(st) ^ mix<RB>(col)) << 4));
-#pragma unroll
-      for (int w = 0; w < KW; ++w) x[w] = M::product(k[w][st], q, x[w]);
-    }
-    const float2 row = row_of[t & 1][col];
-    const int lim = __float_as_int(row.y);
-    if (__any(lim < my_end)) {
-#pragma unroll
-      for (int w = 0; w < KW; ++w)
-#pragma unroll
-        for (int u = 0; u < 16; ++u) {
-          const int key = my_k0 + w * 32 + 8 * (u / 4) + 4 * grp + u % 4;
-          const float y = __builtin_amdgcn_exp2f(fmaf(x[w][u], scale2, -row.x));
-          sum[w][u] += key <= lim ? y : 0.f;
-        }
-    } else {
-#pragma unroll
-      for (int w = 0; w < KW; ++w)
-#pragma unroll
-        for (int u = 0; u < 16; ++u) sum[w][u] += __builtin_amdgcn_exp2f(fmaf(x[w][u], scale2, -row.x));
-    }
-    if ((t - t0) % 16 == 15) {
-#pragma unroll
-      for (int w = 0; w < KW; ++w) total[w] += sum[w], sum[w] = f32x16{};
+    for (int i = 0; i < 2 * S::kLoads; ++i) {
+      const int row = my_row + i * kApart;
+      *reinterpret_cast<u32x4*>(lds + row * RB + ((my_piece ^ mix<RB>(row)) << 4)) = u32x4{0, 0, 0, 0};
     }
   }
 
-  // ---- over the 32 columns: half the values go to the partner lane each time
+  const float scale2 = a.scale * kLog2e;
+  const int my_k0 = k0 + wave * KW * 32, my_end = my_k0 + KW * 32 - 1;
+  // (added up by 32 rows, then by 16 stages, then all: long sums in one go would lose digits)
+  float sum[KW], total[KW];
+#pragma unroll
+  for (int w = 0; w < KW; ++w) sum[w] = total[w] = 0.f;
+  if (t0 < t1) {
+    find_rows(t0);
+    tell_rows(t0);
+    find_rows(t0 + 1);
+    tell_rows(t0 + 1);
+    find_rows(t0 + 2);
+    __syncthreads();
+    load_rows(t0);
+  }
+  for (int t = t0; t < t1; ++t) {
+    store_rows(t);
+    __syncthreads();
+    if (t + 1 < t1) {
+      load_rows(t + 1);
+      tell_rows(t + 2);
+      find_rows(t + 3);
+    }
+    const bool all_seen = !__any(lim_of[t % 3][lane & (S::kRows - 1)] < my_end);
+#pragma unroll
+    for (int half = 0; half < S::kRows / 32; ++half) {
+      const unsigned char* from = lds + (t & 1) * S::kStage + half * 32 * RB;
+      f32x4v less[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) less[i] = less_of[t % 3][half * 8 + 2 * i + grp];
+      u32x4 q[kSteps];
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st) q[st] = *reinterpret_cast<const u32x4*>(from + col * RB + ((piece(st) ^ mix<RB>(col)) << 4));
+      if (all_seen) {
+#pragma unroll
+        for (int w = 0; w < KW; ++w) {
+          f32x16 x = f32x16{};
+#pragma unroll
+          for (int st = 0; st < kSteps; ++st) x = M::product(q[st], k[w][st], x);
+          float y = 0.f;
+#pragma unroll
+          for (int u = 0; u < 16; ++u) y += __builtin_amdgcn_exp2f(fmaf(x[u], scale2, -less[u / 4][u % 4]));
+          sum[w] += y;
+        }
+      } else {
+#pragma unroll
+        for (int w = 0; w < KW; ++w) {
+          f32x16 x = f32x16{};
+#pragma unroll
+          for (int st = 0; st < kSteps; ++st) x = M::product(q[st], k[w][st], x);
+          float y = 0.f;
+#pragma unroll
+          for (int u = 0; u < 16; ++u) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(x[u], scale2, -less[u / 4][u % 4]));
+            y += my_k0 + w * 32 + col <= lim_of[t % 3][half * 32 + 8 * (u / 4) + 4 * grp + u % 4] ? e : 0.f;
+          }
+          sum[w] += y;
+        }
+      }
+    }
+    if ((t - t0) % 16 == 15) {
+#pragma unroll
+      for (int w = 0; w < KW; ++w) total[w] += sum[w], sum[w] = 0.f;
+    }
+  }
+
   __syncthreads();
   float* out = reinterpret_cast<float*>(lds);
 #pragma unroll
   for (int w = 0; w < KW; ++w) {
-    float v[16];
-#pragma unroll
-    for (int u = 0; u < 16; ++u) v[u] = total[w][u] + sum[w][u];
-#pragma unroll
-    for (int half = 8; half >= 1; half /= 2) {
-      const bool high = (col & half) != 0;
-#pragma unroll
-      for (int u = 0; u < half; ++u) {
-        const float give = high ? v[u] : v[u + half], keep = high ? v[u + half] : v[u];
-        v[u] = keep + __shfl_xor(give, half);
-      }
-    }
-    v[0] += __shfl_xor(v[0], 16);
-    const int u = col & 15;
-    if (col < 16) out[wave * KW * 32 + w * 32 + 8 * (u / 4) + 4 * grp + u % 4] = v[0];
+    float y = total[w] + sum[w];
+    y += __shfl_xor(y, 32);
+    if (grp == 0) out[(wave * KW + w) * 32 + col] = y;
   }
   __syncthreads();
   const int key = k0 + (int)threadIdx.x;
@@ -259,6 +290,145 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_gather_weights(Gathe
     sp.sums[(part * blocks + block) * S::kKeys + threadIdx.x] = out[threadIdx.x];
   } else if (key < s.kv) {
     put_weight(a, c, s, head, key, out[threadIdx.x]);
+  }
+}
+
+// A few rows: a wave takes tiles of 16 keys against 16 rows at a time and leaves LDS alone.  All its keys are asked for at once, so
+// that a call of single tokens is bound by memory.  NT: tiles of a wave in registers, a multiple of four.
+template <int DT, int DP, class HELD>
+struct GatherFewShape {
+  static constexpr int kTileRegs = DP / 4 * (HELD::kCodes ? 4 : DT == kBF16 ? 16 : 32) / 32;  // of a tile's keys
+  static constexpr int NT = kTileRegs <= 8 ? 8 : 4;
+  static constexpr int kKeys = 4 * 16 * NT;
+};
+
+template <int DT, int DP, class HELD>
+__global__ __launch_bounds__(256, DT == kF32 && DP == 256 ? 1 : 2) void k_gather_weights_few(Gather a, Cache c, Shares sp, unsigned first) {
+  typedef GatherFewShape<DT, DP, HELD> S;
+  typedef Math<DT, 16> M;
+  constexpr int NT = S::NT, kSteps = M::template steps<DP>(), kMine = DP / 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, grp = lane >> 4, col = lane & 15;
+  const int r = c.Hq / c.Hkv;
+
+  unsigned id = first + blockIdx.x;
+  const int head = (int)(id % (unsigned)c.Hkv);
+  id /= (unsigned)c.Hkv;
+  const int tile = (int)(id % (unsigned)sp.tiles), owner = (int)(id / (unsigned)sp.tiles);
+  const Share s = share_of(c, sp.prefix != 0, owner);
+  if (!s.valid && threadIdx.x == 0 && tile == 0) flag(c, kBadSequence);
+  const int k0 = tile * S::kKeys + wave * 16 * NT, last_key = s.kv - 1;
+  if (!s.valid || s.n <= 0 || k0 >= s.kv) return;
+  const bool causal = a.causal && !sp.prefix;
+  const int rows = s.n * r, row_first = causal ? max(0, k0 - s.fresh) * r : 0, mask = (1 << c.page_shift) - 1;
+
+  // ---- keys: of key `col` of a tile the lane group's pieces of the row, every fourth, or one run of codes
+  auto piece = [&](int st) { return HELD::kCodes ? grp * kSteps + st : 4 * st + grp; };
+  int page[NT], page_out[NT / 4];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) page[t] = s.table[min(k0 + t * 16 + col, last_key) >> c.page_shift];
+  // (the keys that this lane writes: of tile 4 x + col / 4 key 4 grp + col % 4)
+  auto key_out = [&](int x) { return k0 + (4 * x + (col >> 2)) * 16 + 4 * grp + (col & 3); };
+#pragma unroll
+  for (int x = 0; x < NT / 4; ++x) page_out[x] = s.table[min(key_out(x), last_key) >> c.page_shift];
+  bool bad = false;
+  constexpr int kBlocks = kMine > 32 ? kMine / 32 : 1;
+  typedef Codes<(kMine < 32 ? kMine : 32) / 8> Run;
+  u32x4 kr[NT][HELD::kCodes ? 1 : kSteps];
+  Run kc[NT][kBlocks];
+  uint32_t ke[NT][kBlocks];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    bool none = (unsigned)page[t] >= (unsigned)c.n_pages;
+    bad = bad || none;
+    const long at = (none ? 0L : (long)page[t] * c.page_ld) + (long)(min(k0 + t * 16 + col, last_key) & mask) * c.row_ld + (long)head * c.head_ld;
+    if constexpr (HELD::kCodes) {
+#pragma unroll
+      for (int j = 0; j < kBlocks; ++j) {
+        const int v = grp * kMine + j * 32 < c.d ? grp * kMine + j * 32 : 0;  // (past the head: what is there, by queries of zeros)
+        __builtin_memcpy(&kc[t][j], __builtin_assume_aligned(static_cast<const unsigned char*>(a.k_pool) + (at + v) / 2, sizeof(Run)), sizeof(Run));
+        ke[t][j] = a.k_scales[(at + v) / 32];
+      }
+    } else {
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st) {
+        const int e = piece(st) * M::kVec;
+        kr[t][st] = u32x4{0, 0, 0, 0};
+        if (e < c.d) kr[t][st] = *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(a.k_pool) + (at + e) * (16 / M::kVec));
+      }
+    }
+  }
+  if (bad) flag(c, kBadPage);
+  float old[NT / 4];
+  float* put[NT / 4];
+#pragma unroll
+  for (int x = 0; x < NT / 4; ++x) {
+    const bool none = (unsigned)page_out[x] >= (unsigned)c.n_pages || key_out(x) > last_key;
+    put[x] = none ? nullptr : a.weights + (((long)page_out[x] * c.Hkv + head) << c.page_shift) + (key_out(x) & mask);
+    old[x] = a.carry == 0.f || none || key_out(x) >= s.fresh ? 0.f : a.carry * *put[x];
+  }
+
+  const float scale2 = a.scale * kLog2e;
+  float sum[NT][4];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) sum[t][u] = 0.f;
+  for (int row0 = row_first; row0 < rows; row0 += 16) {
+    const int row = row0 + col, have = min(row, rows - 1), tok = (int)(((double)have + 0.5) * a.per_token), qh = head * r + have - tok * r;
+    const float lse = a.lse[(long)(s.tok0 + tok) * c.Hq + qh];
+    const int lim = row >= rows || lse == -INFINITY ? -1 : causal ? min(s.fresh + tok, last_key) : last_key;
+    const unsigned char* q_at = static_cast<const unsigned char*>(a.q) + ((long)(s.tok0 + tok) * a.q_ld + (long)qh * c.d) * (16 / M::kVec);
+    u32x4 q[kSteps];
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st) {
+      const int e = piece(st) * M::kVec;
+      q[st] = u32x4{0, 0, 0, 0};
+      if (e < c.d && a.scale != 0.f) q[st] = *reinterpret_cast<const u32x4*>(q_at + e * (16 / M::kVec));
+    }
+    const float lse2 = lse * kLog2e;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      if constexpr (HELD::kCodes) {
+#pragma unroll
+        for (int j = 0; j < kBlocks; ++j) made_here(ke[t][j]);
+      }
+      f32x4v x = {};
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st) {
+        u32x4 k;
+        if constexpr (HELD::kCodes) {
+          constexpr int kPer = kMine < 32 ? kSteps : 32 / M::kVec;
+          k = HELD::template piece<DT>(kc[t][st / kPer].v[st % kPer * M::kVec / 8], ke[t][st / kPer], st * M::kVec / 4 % 2);
+        } else {
+          k = kr[t][st];
+        }
+        x = M::qk(k, q[st], x);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float y = __builtin_amdgcn_exp2f(fmaf(x[u], scale2, -lse2));
+        sum[t][u] += k0 + t * 16 + 4 * grp + u <= lim ? y : 0.f;
+      }
+    }
+  }
+  // ---- over the 16 columns, by rotations of them; then every lane has the four sums of each tile
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      float y = sum[t][u];
+      y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x128, 0xf, 0xf, true));
+      y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x124, 0xf, 0xf, true));
+      y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x122, 0xf, 0xf, true));
+      y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x121, 0xf, 0xf, true));
+      sum[t][u] = y;
+    }
+#pragma unroll
+  for (int x = 0; x < NT / 4; ++x) {
+    float mine = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mine = col == i ? sum[4 * x + i / 4][i % 4] : mine;
+    if (put[x] != nullptr) *put[x] = mine + old[x];
   }
 }
 
