@@ -144,10 +144,10 @@ namespace dart {
 dart_status dart_attend_join(const Attend& a, const Cache& c, int dtype, const AttendPlan& p, hipStream_t st) {
   const JoinPlan j = plan_join(c, p.parts);
   if (dtype == DART_BF16)
-    k_attend_join<kBF16><<<dim3((unsigned)j.blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, p.own.part_o,
+    k_attend_join<kBF16><<<dim3((unsigned)j.blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, p.own.share, p.own.part_o,
                                                                         p.own.part_ml, j.lanes_shift, j.split_shift);
   else
-    k_attend_join<kF32><<<dim3((unsigned)j.blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, p.own.part_o,
+    k_attend_join<kF32><<<dim3((unsigned)j.blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, p.own.share, p.own.part_o,
                                                                        p.own.part_ml, j.lanes_shift, j.split_shift);
   return launched();
 }

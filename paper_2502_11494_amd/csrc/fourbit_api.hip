@@ -22,11 +22,12 @@ dart_status check_pool(const void* codes, const void* scales) {
 
 template <int DT, bool READ>
 dart_status launch_hold(const Hold& a, const Cache& c, hipStream_t st) {
-  // Four waves share a token where there are few, or where each then has two rounds of blocks or more.
-  if (a.T < 1024 || (2 * a.heads_blocks >= 8 * 16 && a.T < kMaxTokens))
-    k_hold<DT, 4, READ><<<dim3(a.T), dim3(256), 0, st>>>(a, c);
+  // Four waves share a token where there are few; else each has its own, whose place it then finds once for all heads (23 040 tokens
+  // of 32 + 32 heads, bf16: append and read 94 + 70 us, with four waves 113 + 71).
+  if (a.T < 1024)
+    k_hold<DT, 4, READ><<<dim3((unsigned)round_up8(a.T)), dim3(256), 0, st>>>(a, c);
   else
-    k_hold<DT, 1, READ><<<dim3((a.T + 3) / 4), dim3(256), 0, st>>>(a, c);
+    k_hold<DT, 1, READ><<<dim3((unsigned)round_up8((a.T + 3) / 4)), dim3(256), 0, st>>>(a, c);
   return launched();
 }
 
@@ -56,7 +57,7 @@ dart_status launch_tiles(const Attend& a, const Cache& c, const Parting& sp, hip
 template <int DT, int DP>
 dart_status launch_attend(const Attend& a, const Cache& c, const Parting& sp, Kind kind, hipStream_t st) {
   if constexpr (DP <= 128)
-    if (kind == kFew && c.page_shift >= 4 && c.row_16 < 1u << 24) return launch_tiles<DT, DP, 16, 1, 4, 64, In4BitsPages>(a, c, sp, st);
+    if (kind == kFew && codes_in_pages(c, true)) return launch_tiles<DT, DP, 16, 1, 4, 64, In4BitsPages>(a, c, sp, st);
   if constexpr (DT == kBF16 || DP <= 128)
     if (kind == kFew) return launch_tiles<DT, DP, 16, 1, 4, 32>(a, c, sp, st);
   if constexpr (DT == kBF16 && DP <= 128)

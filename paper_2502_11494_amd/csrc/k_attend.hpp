@@ -41,7 +41,8 @@ __device__ __forceinline__ int token_in(const Attend& a, int row) { return (int)
 struct Parting {
   int prefix;      // the keys are the groups' shared prefixes (else each sequence's own)
   int few;         // tiles of 16 rows, the keys dealt to four waves (else four waves of rows)
-  int chunk;       // keys of a part
+  int chunk;       // keys of a part; the least, where `share` is not 0
+  int share;       // parts that all sequences together are to have (see part_keys), or 0
   int chunks;
   int first_part;  // part number of the first chunk
   int parts;
@@ -50,6 +51,18 @@ struct Parting {
   float* part_o;   // [parts][T*Hq][d]
   float2* part_ml; // [parts][T*Hq]: maximum (of scores times log2 e), sum
 };
+
+// Keys of a part.  The host knows the longest sequence only; where lengths differ, parts cut for it leave some units without work.
+// With `share` not 0 (64 sequences at most) every wave adds the lengths up and cuts all of them alike, for about so many parts.
+__device__ __forceinline__ int part_keys(const Cache& c, int chunk, int share) {
+  if (share == 0) return chunk;
+  const int lane = threadIdx.x & 63, kv = lane < c.B ? c.kv_len[lane] : 0;
+  int units = kv > 0 && kv <= c.max_kv ? (kv + 255) / 256 : 0;  // (2^25 of all)
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) units += __shfl_xor(units, o);
+  const int per = (units + share - 1) / share * 256;
+  return __builtin_amdgcn_readfirstlane(per > chunk ? per : chunk);
+}
 
 // ---- the arithmetic of a wave ----------------------------------------------------------------
 // QW queries (32, or 16 where a block has no more) lie in the columns of a matrix tile, lane % QW, and its
@@ -292,8 +305,9 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   const bool causal = a.causal && !sp.prefix;
   int k1 = kv;
   if (causal) k1 = min(kv, kv - n + token_in(a, min(row0 + S::kBM, rows) - 1) + 1);
-  const int k0 = part * sp.chunk;
-  k1 = min(k1, k0 + sp.chunk);
+  const int chunk = HELD::kPages ? part_keys(c, sp.chunk, sp.share) : sp.chunk;
+  const int k0 = part * chunk;
+  k1 = min(k1, k0 + chunk);
   if (k1 <= k0 && (sp.parts > 1 || part > 0)) return;
 
   // ---- staging: pieces of keys and values, through registers into LDS.  Loads are unconditional: what lies
@@ -889,11 +903,12 @@ __global__ __launch_bounds__(256, DT == kBF16 && DP <= 128 ? 2 : 1) void k_atten
 // parts are asked for at once: eight, of which those past the last are read in vain, take 2 us more there and gain nothing
 // with 63 parts.
 template <int DT>
-__global__ __launch_bounds__(256) void k_attend_join(Attend a, Cache c, int pre_chunk, int pre_parts, int own_chunk, const float* part_o,
+__global__ __launch_bounds__(256) void k_attend_join(Attend a, Cache c, int pre_chunk, int pre_parts, int own_least, int own_share, const float* part_o,
                                                      const float2* part_ml, int lanes_shift, int split_shift) {
   __shared__ f32x4v set_x[256];
   __shared__ float2 set_ml[256];
   const int all = c.T * c.Hq;  // (2^24 at most)
+  const int own_chunk = part_keys(c, own_least, own_share);
   const int lane = threadIdx.x & 63, set = threadIdx.x >> lanes_shift, sub = set & ((1 << split_shift) - 1);
   const int rows_shift = 8 - lanes_shift - split_shift;  // rows of a block
   const int first = (int)blockIdx.x << rows_shift, id = first + (set >> split_shift);
@@ -1007,6 +1022,9 @@ __global__ __launch_bounds__(256) void k_attend_join(Attend a, Cache c, int pre_
 // ---- attention: which tiles, how many parts ---------------------------------------------------
 enum Kind { kFew, kMany, kWide };  // 16 rows, the keys dealt to four waves; four waves of rows; eight
 
+// Pages that hold whole tiles of 16 keys, their rows near enough for offsets of 32 bits.
+inline bool codes_in_pages(const Cache& c, bool codes) { return codes && c.d <= 128 && c.page_shift >= 4 && c.row_16 < 1u << 24; }
+
 struct AttendPlan {
   Kind own_kind, pre_kind;
   Parting own, pre;
@@ -1061,11 +1079,20 @@ inline Kind plan_parting(const Cache& c, int dtype, bool prefix, long rows, int 
   return kind;
 }
 
+// (codes: the pools are held in 4 bits)
 inline dart_status plan_attend(const Cache& c, int dtype, AttendPlan& p, bool codes = false) {
   const int r = c.Hq / c.Hkv;
   if ((long)c.T * r > kMaxRows) return DART_ERR_SHAPE;
   p = {};
   p.own_kind = plan_parting(c, dtype, false, (long)c.max_q * r, c.B, c.max_kv, p.own, codes);
+  if (codes_in_pages(c, codes) && p.own_kind == kFew && (long)c.max_q * r <= 16 && c.groups == 0 && c.B > 1 && c.B <= kWave && p.own.chunks > 1) {
+    // (32 tokens over 1024 to 16 384 keys, 28 + 4 heads: 45 us, 50 with parts cut for the longest; 32 over 8704 each 38 and 36.)
+    // Two blocks to a unit, half a part to each key head of a sequence left for its last one, which is shorter; the cut may come to a
+    // quarter of what the longest sequence alone would ask for.
+    p.own.share = std::max(1L, (512L - (long)c.B * c.Hkv / 2) / c.Hkv);
+    p.own.chunk = std::max(256, (p.own.chunk / 4 + 255) / 256 * 256);
+    p.own.chunks = (c.max_kv + p.own.chunk - 1) / p.own.chunk;
+  }
   p.parts = p.own.chunks;
   if (c.groups > 0) {
     const long rows = std::min((long)c.T, (long)c.max_q * c.B) * r;

@@ -14,6 +14,12 @@ __global__ __launch_bounds__(64 * WM * WK, HELD::kPages && DT == kBF16 ? 3 : DP 
   long slot;
   int head, part;
   attend_place(c, sp, blockIdx.x, slot, head, part);
+  if (HELD::kPages && sp.share != 0) {  // (the parts that no sequence has come last)
+    const unsigned rows = (unsigned)sp.slots * (unsigned)c.Hkv, rest = blockIdx.x % rows;
+    part = (int)(blockIdx.x / rows);
+    head = (int)(rest % (unsigned)c.Hkv);
+    slot = (long)(rest / (unsigned)c.Hkv);
+  }
   attend_tile<DT, DP, QW, WM, WK, KT, HELD>(a, c, sp, lds, sh, slot, head, part);
 }
 

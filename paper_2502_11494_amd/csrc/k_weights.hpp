@@ -238,15 +238,18 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_gather_weights(Gathe
       f32x4v less[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) less[i] = less_of[t % 3][half * 8 + 2 * i + grp];
-      u32x4 q[kSteps];
+      auto read_row = [&](int st) { return *reinterpret_cast<const u32x4*>(from + col * RB + ((piece(st) ^ mix<RB>(col)) << 4)); };
+      u32x4 q[kSteps];  // (for several tiles of keys; one takes them as they come)
+      if (KW > 1) {
 #pragma unroll
-      for (int st = 0; st < kSteps; ++st) q[st] = *reinterpret_cast<const u32x4*>(from + col * RB + ((piece(st) ^ mix<RB>(col)) << 4));
+        for (int st = 0; st < kSteps; ++st) q[st] = read_row(st);
+      }
       if (all_seen) {
 #pragma unroll
         for (int w = 0; w < KW; ++w) {
           f32x16 x = f32x16{};
 #pragma unroll
-          for (int st = 0; st < kSteps; ++st) x = M::product(q[st], k[w][st], x);
+          for (int st = 0; st < kSteps; ++st) x = M::product(KW > 1 ? q[st] : read_row(st), k[w][st], x);
           float y = 0.f;
 #pragma unroll
           for (int u = 0; u < 16; ++u) y += __builtin_amdgcn_exp2f(fmaf(x[u], scale2, -less[u / 4][u % 4]));
@@ -257,7 +260,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_gather_weights(Gathe
         for (int w = 0; w < KW; ++w) {
           f32x16 x = f32x16{};
 #pragma unroll
-          for (int st = 0; st < kSteps; ++st) x = M::product(q[st], k[w][st], x);
+          for (int st = 0; st < kSteps; ++st) x = M::product(KW > 1 ? q[st] : read_row(st), k[w][st], x);
           float y = 0.f;
 #pragma unroll
           for (int u = 0; u < 16; ++u) {
@@ -294,17 +297,16 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_gather_weights(Gathe
 }
 
 // A few rows: a wave takes tiles of 16 keys against 16 rows at a time and leaves LDS alone.  All its keys are asked for at once, so
-// that a call of single tokens is bound by memory.  NT: tiles of a wave in registers, a multiple of four.
-template <int DT, int DP, class HELD>
+// that a call of single tokens is bound by memory.  NT: tiles of a wave (32 tokens over 1024 to 16 384 keys
+// held in 4 bits 26.4 us, with eight 29).
 struct GatherFewShape {
-  static constexpr int kTileRegs = DP / 4 * (HELD::kCodes ? 4 : DT == kBF16 ? 16 : 32) / 32;  // of a tile's keys
-  static constexpr int NT = kTileRegs <= 8 ? 8 : 4;
+  static constexpr int NT = 4;
   static constexpr int kKeys = 4 * 16 * NT;
 };
 
 template <int DT, int DP, class HELD>
 __global__ __launch_bounds__(256, DT == kF32 && DP == 256 ? 1 : 2) void k_gather_weights_few(Gather a, Cache c, Shares sp, unsigned first) {
-  typedef GatherFewShape<DT, DP, HELD> S;
+  typedef GatherFewShape S;
   typedef Math<DT, 16> M;
   constexpr int NT = S::NT, kSteps = M::template steps<DP>(), kMine = DP / 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, grp = lane >> 4, col = lane & 15;

@@ -24,6 +24,11 @@ inline int atomicAdd(int* p, int v) {
   return old;
 }
 
+// (common.hpp has it for the device's compiler only)
+namespace dart {
+inline long xcd_contiguous(unsigned block, unsigned blocks) { return (long)(block % 8) * (blocks / 8) + block / 8; }
+}
+
 // 4-bit values and their scales, by their definition.
 typedef __bf16 lanes_bf2 __attribute__((ext_vector_type(2)));
 typedef float lanes_f2 __attribute__((ext_vector_type(2)));
