@@ -467,13 +467,13 @@ def _cache(Hq, d, kind, pool, values, pages, kv_len, max_kv, T, max_q, cu_q, gro
         c.max_prefix = room if max_prefix is None else max_prefix if c.prefix_n else 0
     c._keepalive = (pages, kv_len, cu_q, group_cu, prefix_pages, prefix_len)
     c._ref, c._heads = C.byref(c), (kind, Hq, c.Hkv, c.d, c.T)
-    c._pool, c._kind, c._scales = (pool.shape, pool.stride()), pool.dtype, None
+    c._pool, c._scales = (pool.shape, pool.stride()), None
     return c
 
 
 def _pool(cache: DartCache, p, what: str):
     shape, stride = cache._pool
-    if p.shape != shape or p.dtype is not cache._kind or (
+    if not isinstance(p, torch.Tensor) or p.shape != shape or p.dtype is not cache._heads[0] or (
             p.stride() != stride and any(a != b for a, b, n in zip(p.stride(), stride, shape) if n > 1)):
         raise ValueError(f"{what}: shape, strides and dtype of the pool the descriptor was made for")
     return p.data_ptr()
@@ -588,24 +588,25 @@ def make_cache_4bit(Hq: int, d: int, dtype: int, pool, pages: torch.Tensor, kv_l
     return c
 
 
-def _held(cache: DartCache, p, what: str):
-    """Addresses of (codes, scales), or of a pool of rows and None."""
-    if cache._scales is None:
-        return _pool(cache, p, what), None
-    if not isinstance(p, (tuple, list)) or len(p) != 2:
-        raise ValueError(f"{what}: (codes, scales)")
-    codes, scales = p
-    shape, stride = cache._scales
-    if scales.shape != shape or scales.dtype is not torch.uint8 or (
-            scales.stride() != stride and any(a != b for a, b, n in zip(scales.stride(), stride, shape) if n > 1)):
-        raise ValueError(f"{what}: scales as of the pool the descriptor was made for")
-    return _pool(cache, codes, what), scales.data_ptr()
+def _alike(t, like) -> bool:
+    """uint8, of this shape and strides (where they count)."""
+    shape, stride = like
+    return t.dtype is torch.uint8 and t.shape == shape and (
+        t.stride() == stride or all(a == b for a, b, n in zip(t.stride(), stride, shape) if n > 1))
 
 
 def _codes(cache: DartCache, p, what: str):
+    """Addresses of (codes, scales)."""
     if cache._scales is None:
         raise ValueError("cache: of make_cache_4bit")
-    return _held(cache, p, what)
+    if not isinstance(p, (tuple, list)) or len(p) != 2 or not _alike(p[0], cache._pool) or not _alike(p[1], cache._scales):
+        raise ValueError(f"{what}: (codes, scales) as of the pool the descriptor was made for")
+    return p[0].data_ptr(), p[1].data_ptr()
+
+
+def _held(cache: DartCache, p, what: str):
+    """Addresses of (codes, scales), or of a pool of rows and None."""
+    return (_pool(cache, p, what), None) if cache._scales is None else _codes(cache, p, what)
 
 
 def _workspace(n: int, where: str, device):
