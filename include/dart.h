@@ -509,7 +509,8 @@ DART_API dart_status dart_attend(const dart_cache* cache, const void* q, int64_t
  * it stands there.                                                                            */
 
 /* Writes key and value rows (laid out as in dart_norm_rotate_append, keys turned already) to their places in 4-bit pages:
- * token i of sequence b becomes key kv_len[b] - n_b + i, so kv_len[b] >= n_b is required. */
+ * token i of sequence b becomes key kv_len[b] - n_b + i, so kv_len[b] >= n_b is required.  A row of a page that two tokens of
+ * a call name gets codes and scales of either. */
 DART_API dart_status dart_append_4bit(const dart_cache* cache, const void* k, int64_t k_ld, const void* v, int64_t v_ld,
                                       void* k_codes, void* k_scales, void* v_codes, void* v_scales, int32_t* status,
                                       void* stream);
@@ -546,7 +547,8 @@ DART_API size_t dart_attend_weights_workspace_bytes(const dart_cache* cache, int
  * to it or came from it.  Keys that belong to the call's tokens start from 0, whatever their weight was, and with carry 0
  * all do (what was there is not read).  A pair whose lse is -infinity gives nothing; another one that is no number, or
  * infinite, goes into the weights of the keys it sees.  The weights of a sequence (or group) without tokens, and of one that is
- * skipped, are left as they were; a group with a sequence that is skipped is skipped.  Sums in 32 bits, in a fixed order; a
+ * skipped, are left as they were; a group with a sequence that is skipped is skipped.  A key that two sequences (or a sequence
+ * and a prefix) of the call have gets what either gives.  Sums in 32 bits, in a fixed order; a
  * factor is as good as lse is, 2^-24 of its magnitude.  scale and carry are finite.  T * (Hq/Hkv) is at most 2^28, and
  * B * Hkv times max_kv in tiles of 128 keys at most 2^30 (beyond: DART_ERR_SHAPE, and 0 bytes of workspace). */
 DART_API dart_status dart_attend_weights(const dart_cache* cache, const void* q, int64_t q_ld, const void* k_pool,

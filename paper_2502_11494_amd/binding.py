@@ -707,11 +707,13 @@ def dart_attend_weights(cache: DartCache, q, k_pool, lse, weights, ws, *, scale:
         _check(rc, "dart_attend_weights")
 
 
-def make_eviction(*, budget: int = 0, ratio=(0, 1), first: int = 0, recent: int = 0) -> DartEviction:
-    """Keys that a sequence keeps: `budget`, or ratio[0]/ratio[1] of its keys where that is 0; the first and the recent ones
+def make_eviction(*, budget: int = 0, ratio=None, first: int = 0, recent: int = 0) -> DartEviction:
+    """Keys that a sequence keeps: `budget`, or where that is 0 ratio[0]/ratio[1] of its keys; the first and the recent ones
     always."""
+    if budget == 0 and ratio is None:
+        raise ValueError("budget or ratio")
     e = DartEviction()
-    e.budget, e.ratio_num, e.ratio_den, e.first, e.recent = budget, ratio[0], ratio[1], first, recent
+    e.budget, (e.ratio_num, e.ratio_den), e.first, e.recent = budget, ratio or (0, 1), first, recent
     e._ref = C.byref(e)
     return e
 

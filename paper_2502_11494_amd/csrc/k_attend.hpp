@@ -60,7 +60,7 @@ __device__ __forceinline__ int part_keys(const Cache& c, int chunk, int share) {
   int units = kv > 0 && kv <= c.max_kv ? (kv + 255) / 256 : 0;  // (2^25 of all)
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) units += __shfl_xor(units, o);
-  const int per = (units + share - 1) / share * 256;
+  const int per = min((units + share - 1) / share, 1 << 19) * 256;  // (no sequence has more keys)
   return __builtin_amdgcn_readfirstlane(per > chunk ? per : chunk);
 }
 
@@ -306,7 +306,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   int k1 = kv;
   if (causal) k1 = min(kv, kv - n + token_in(a, min(row0 + S::kBM, rows) - 1) + 1);
   const int chunk = HELD::kPages ? part_keys(c, sp.chunk, sp.share) : sp.chunk;
-  const int k0 = part * chunk;
+  const int k0 = HELD::kPages ? (int)min((long)part * chunk, (long)k1) : part * chunk;  // (a part that no sequence has may lie anywhere)
   k1 = min(k1, k0 + chunk);
   if (k1 <= k0 && (sp.parts > 1 || part > 0)) return;
 
@@ -1089,9 +1089,12 @@ inline dart_status plan_attend(const Cache& c, int dtype, AttendPlan& p, bool co
     // (32 tokens over 1024 to 16 384 keys, 28 + 4 heads: 45 us, 50 with parts cut for the longest; 32 over 8704 each 38 and 36.)
     // Two blocks to a unit, half a part to each key head of a sequence left for its last one, which is shorter; the cut may come to a
     // quarter of what the longest sequence alone would ask for.
-    p.own.share = std::max(1L, (512L - (long)c.B * c.Hkv / 2) / c.Hkv);
-    p.own.chunk = std::max(256, (p.own.chunk / 4 + 255) / 256 * 256);
-    p.own.chunks = (c.max_kv + p.own.chunk - 1) / p.own.chunk;
+    const int chunk = std::max(256, (p.own.chunk / 4 + 255) / 256 * 256), chunks = (c.max_kv + chunk - 1) / chunk;
+    if (p.own.slots * c.Hkv * chunks <= kMaxBlocks) {  // (in one launch)
+      p.own.share = std::max(1L, (512L - (long)c.B * c.Hkv / 2) / c.Hkv);
+      p.own.chunk = chunk;
+      p.own.chunks = chunks;
+    }
   }
   p.parts = p.own.chunks;
   if (c.groups > 0) {

@@ -85,6 +85,8 @@ def share():
             launches = run(c, f"share {dtype} {d} {max_kv}", max_kv=max_kv)
             assert "join" in launches
         run(U.make([2, 0, 1, 3], [1500, 3, 1, 700], 4, 1, d, 32, dtype, seed=d), f"share, packed {dtype} {d}", max_kv=3000, ld=2)
+    # a bound as far as it goes: many parts that no sequence has, their numbers times the keys of one beyond 32 bits
+    run(U.make([1, 1], [9000, 2000], 1, 1, 8, 16, "bf16", seed=5), "share, far bound", max_kv=2 ** 22)
 
 
 def weigh(c, name, scale=0.11, causal=True, carry=0.5, **how):

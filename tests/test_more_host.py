@@ -169,6 +169,8 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
     plain = D.make_cache(4, rows, pages, kv, 32)
     e = D.make_eviction(budget=8)
     assert D.dart_evict_most(c, e) == D.dart_evict_most(plain, e) == 8
+    with pytest.raises(ValueError):
+        D.make_eviction(first=4)  # (which would keep nothing else)
     with pytest.raises(D.DartError):
         D.dart_evict_most(c, D.make_eviction(budget=-1))
     with pytest.raises(D.DartError):
