@@ -141,15 +141,21 @@ dart_status launch_attend(const Attend& a, const Cache& c, int dtype, const Part
 
 namespace dart {
 
-dart_status dart_attend_join(const Attend& a, const Cache& c, int dtype, const AttendPlan& p, hipStream_t st) {
+// (SHARED: the own keys' parts are cut on the device; what reads them pays for that only then)
+template <bool SHARED>
+dart_status dart_attend_join_of(const Attend& a, const Cache& c, int dtype, const AttendPlan& p, hipStream_t st) {
   const JoinPlan j = plan_join(c, p.parts);
   if (dtype == DART_BF16)
-    k_attend_join<kBF16><<<dim3((unsigned)j.blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, p.own.share, p.own.part_o,
-                                                                        p.own.part_ml, j.lanes_shift, j.split_shift);
+    k_attend_join<kBF16, SHARED><<<dim3((unsigned)j.blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, p.own.share,
+                                                                                p.own.part_o, p.own.part_ml, j.lanes_shift, j.split_shift);
   else
-    k_attend_join<kF32><<<dim3((unsigned)j.blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, p.own.share, p.own.part_o,
-                                                                       p.own.part_ml, j.lanes_shift, j.split_shift);
+    k_attend_join<kF32, SHARED><<<dim3((unsigned)j.blocks), dim3(256), 0, st>>>(a, c, p.pre.chunk, p.pre.chunks, p.own.chunk, p.own.share,
+                                                                               p.own.part_o, p.own.part_ml, j.lanes_shift, j.split_shift);
   return launched();
+}
+
+dart_status dart_attend_join(const Attend& a, const Cache& c, int dtype, const AttendPlan& p, hipStream_t st) {
+  return p.own.share > 0 ? dart_attend_join_of<true>(a, c, dtype, p, st) : dart_attend_join_of<false>(a, c, dtype, p, st);
 }
 
 }  // namespace dart

@@ -41,13 +41,13 @@ void set_hold(Hold& a, const Cache& c) {
 }
 
 template <int DT, int DP, int QW, int WM, int WK, int KT, class HELD = In4Bits>
-dart_status launch_tiles(const Attend& a, const Cache& c, const Parting& sp, hipStream_t st) {
+dart_status launch_tiles(const Attend& a, const Scales& scales, const Cache& c, const Parting& sp, hipStream_t st) {
   typedef AttendShape<DT, DP, QW, WM, WK, KT, HELD> S;
   const long most = kMaxBlocks / ((long)c.Hkv * sp.chunks);
   Parting left = sp;
   while (left.slots > 0) {
     const long slots = std::min(left.slots, most);
-    k_attend_4bit<DT, DP, QW, WM, WK, KT, HELD><<<dim3((unsigned)(slots * c.Hkv * sp.chunks)), dim3(S::kThreads), S::kLds, st>>>(a, c, left);
+    k_attend_4bit<DT, DP, QW, WM, WK, KT, HELD><<<dim3((unsigned)(slots * c.Hkv * sp.chunks)), dim3(S::kThreads), S::kLds, st>>>(a, scales, c, left);
     DART_TRY(launched());
     left.slots -= slots;
   }
@@ -55,38 +55,38 @@ dart_status launch_tiles(const Attend& a, const Cache& c, const Parting& sp, hip
 }
 
 template <int DT, int DP>
-dart_status launch_attend(const Attend& a, const Cache& c, const Parting& sp, Kind kind, hipStream_t st) {
+dart_status launch_attend(const Attend& a, const Scales& scales, const Cache& c, const Parting& sp, Kind kind, hipStream_t st) {
   if constexpr (DP <= 128)
-    if (kind == kFew && codes_in_pages(c, true)) return launch_tiles<DT, DP, 16, 1, 4, 64, In4BitsPages>(a, c, sp, st);
+    if (kind == kFew && codes_in_pages(c, true)) return launch_tiles<DT, DP, 16, 1, 4, 64, In4BitsPages>(a, scales, c, sp, st);
   if constexpr (DT == kBF16 || DP <= 128)
-    if (kind == kFew) return launch_tiles<DT, DP, 16, 1, 4, 32>(a, c, sp, st);
+    if (kind == kFew) return launch_tiles<DT, DP, 16, 1, 4, 32>(a, scales, c, sp, st);
   if constexpr (DT == kBF16 && DP <= 128)
-    if (kind == kWide) return launch_tiles<DT, DP, 32, 8, 1, 64>(a, c, sp, st);
-  return launch_tiles<DT, DP, many_columns(DT, DP), 4, 1, DT == kBF16 ? 64 : 32>(a, c, sp, st);
+    if (kind == kWide) return launch_tiles<DT, DP, 32, 8, 1, 64>(a, scales, c, sp, st);
+  return launch_tiles<DT, DP, many_columns(DT, DP), 4, 1, DT == kBF16 ? 64 : 32>(a, scales, c, sp, st);
 }
 
 template <int DT, int DP>
-dart_status launch_both(const Attend& a, const Cache& c, const Parting& pre, const Parting& own, hipStream_t st) {
+dart_status launch_both(const Attend& a, const Scales& scales, const Cache& c, const Parting& pre, const Parting& own, hipStream_t st) {
   constexpr int KT = DT == kBF16 ? 64 : 32;
   constexpr int kLds = std::max(AttendShape<DT, DP, 16, 1, 4, 32, In4Bits>::kLds, AttendShape<DT, DP, many_columns(DT, DP), 4, 1, KT, In4Bits>::kLds);
   const long n = blocks_of(c, pre);
-  k_attend_4bit_both<DT, DP, KT><<<dim3((unsigned)(n + blocks_of(c, own))), dim3(256), kLds, st>>>(a, c, pre, own, (unsigned)n);
+  k_attend_4bit_both<DT, DP, KT><<<dim3((unsigned)(n + blocks_of(c, own))), dim3(256), kLds, st>>>(a, scales, c, pre, own, (unsigned)n);
   return launched();
 }
 
 template <int DT, int DP>
-dart_status launch_width(const Attend& a, const Cache& c, const AttendPlan& p, hipStream_t st) {
+dart_status launch_width(const Attend& a, const Scales& scales, const Cache& c, const AttendPlan& p, hipStream_t st) {
   if constexpr (DT == kBF16 || DP <= 128)
-    if (p.both) return launch_both<DT, DP>(a, c, p.pre, p.own, st);
-  if (c.groups > 0) DART_TRY((launch_attend<DT, DP>(a, c, p.pre, p.pre_kind, st)));
-  return launch_attend<DT, DP>(a, c, p.own, p.own_kind, st);
+    if (p.both) return launch_both<DT, DP>(a, scales, c, p.pre, p.own, st);
+  if (c.groups > 0) DART_TRY((launch_attend<DT, DP>(a, scales, c, p.pre, p.pre_kind, st)));
+  return launch_attend<DT, DP>(a, scales, c, p.own, p.own_kind, st);
 }
 
 template <int DT>
-dart_status launch_all(const Attend& a, const Cache& c, const AttendPlan& p, hipStream_t st) {
-  DART_TRY((c.d <= 64    ? launch_width<DT, 64>(a, c, p, st)
-            : c.d <= 128 ? launch_width<DT, 128>(a, c, p, st)
-                         : launch_width<DT, 256>(a, c, p, st)));
+dart_status launch_all(const Attend& a, const Scales& scales, const Cache& c, const AttendPlan& p, hipStream_t st) {
+  DART_TRY((c.d <= 64    ? launch_width<DT, 64>(a, scales, c, p, st)
+            : c.d <= 128 ? launch_width<DT, 128>(a, scales, c, p, st)
+                         : launch_width<DT, 256>(a, scales, c, p, st)));
   if (p.parts == 1) return DART_OK;
   return dart_attend_join(a, c, DT == kBF16 ? DART_BF16 : DART_F32, p, st);
 }
@@ -159,12 +159,12 @@ dart_status dart_attend_4bit(const dart_cache* cache, const void* q, int64_t q_l
   DART_TRY(plan_attend(c, cache->dtype, p, true));
   if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < p.total) return DART_ERR_WORKSPACE;
   c.status = status;
-  const Attend a = {q, k_codes, v_codes, out, lse, q_ld, out_ld, scale, causal != 0, 1.0 / (c.Hq / c.Hkv),
-                    static_cast<const uint8_t*>(k_scales), static_cast<const uint8_t*>(v_scales)};
+  const Attend a = {q, k_codes, v_codes, out, lse, q_ld, out_ld, scale, causal != 0, 1.0 / (c.Hq / c.Hkv)};
+  const Scales scales = {static_cast<const uint8_t*>(k_scales), static_cast<const uint8_t*>(v_scales)};
   p.own.part_o = p.pre.part_o = static_cast<float*>(ws);
   p.own.part_ml = p.pre.part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(ws) + p.o_ml);
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  return cache->dtype == DART_BF16 ? launch_all<kBF16>(a, c, p, st) : launch_all<kF32>(a, c, p, st);
+  return cache->dtype == DART_BF16 ? launch_all<kBF16>(a, scales, c, p, st) : launch_all<kF32>(a, scales, c, p, st);
 }
 
 }  // extern "C"

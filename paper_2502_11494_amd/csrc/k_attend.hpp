@@ -29,7 +29,11 @@ struct Attend {
   float scale;
   int causal;
   double per_token;  // 1 / (rows of a token: query heads of a key head)
-  const uint8_t *k_scales, *v_scales;  // (keys and values held in 4 bits: their pools are codes, these the blocks' scales)
+};
+
+// Keys and values held in 4 bits: their pools are codes, these the blocks' scales.
+struct Scales {
+  const uint8_t *k, *v;
 };
 
 // row / rows of a token, exactly: rows are below 2^28.
@@ -254,7 +258,7 @@ struct AttendShared {
 // One block: row tile `slot` against chunk `part` of the keys of head `head`.
 template <int DT, int DP, int QW, int WM, int WK, int KT, class HELD = AsRows>
 __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, const Parting& sp, unsigned char* lds, AttendShared& sh,
-                                            long slot, int head, int part) {
+                                            long slot, int head, int part, const Scales& scales = Scales{}) {
   typedef AttendShape<DT, DP, QW, WM, WK, KT, HELD> S;
   typedef Math<DT, QW> M;
   typedef typename M::acc acc;
@@ -316,11 +320,11 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   const int my_row = gt / S::kPieces, my_piece = gt % S::kPieces;
   const bool my_on = my_piece * S::kUnit < c.d;
   const long my_at = (long)head * c.head_ld + (my_on ? my_piece * S::kUnit : 0);
-  const long piece_at = HELD::kCodes ? my_at / 2 : my_at * S::kEsz;
+  const long piece_at = HELD::kCodes ? my_at / 2 : ((long)head * c.head_ld + (my_on ? my_piece * M::kVec : 0)) * S::kEsz;
   const unsigned char* kp = static_cast<const unsigned char*>(a.k_pool) + piece_at;
   const unsigned char* vp = static_cast<const unsigned char*>(a.v_pool) + piece_at;
-  const uint8_t* ks = HELD::kCodes ? a.k_scales + my_at / 32 : nullptr;
-  const uint8_t* vs = HELD::kCodes ? a.v_scales + my_at / 32 : nullptr;
+  const uint8_t* ks = HELD::kCodes ? scales.k + my_at / 32 : nullptr;
+  const uint8_t* vs = HELD::kCodes ? scales.v + my_at / 32 : nullptr;
   unsigned char* const my_lds = lds + wk * (S::kBuffers * S::kBufferBytes);
   const int row_mask = (1 << c.page_shift) - 1, last_key = k1 - 1;
   typedef typename std::conditional<HELD::kCodes, Codes<S::kUnit / 8 ? S::kUnit / 8 : 1>, u32x4>::type Load;
@@ -339,7 +343,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   const bool group_on = grp * kMine < c.d;
   const long direct_at = (long)head * c.head_ld + (group_on ? grp * kMine : 0);
   const unsigned char* dkp = static_cast<const unsigned char*>(a.k_pool) + direct_at / 2;
-  const uint8_t* dks = S::kDirect ? a.k_scales + direct_at / 32 : nullptr;
+  const uint8_t* dks = S::kDirect ? scales.k + direct_at / 32 : nullptr;
   auto direct_on = [&](int j) { return group_on && grp * kMine + j * 32 < c.d; };
   auto load_pages = [&](int kb) {
 #pragma unroll
@@ -354,15 +358,20 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
     int page = pg[i];
     if ((unsigned)page >= (unsigned)c.n_pages) page = 0, bad_page = true;
     const uint32_t row = min(kb + my_row + i * S::kApart, last_key) & row_mask;
-    return (uint64_t)(uint32_t)page * c.page_16 + (uint64_t)row * c.row_16;
+    // (in bytes; of codes in units of 16 bytes, which are those of a scale)
+    if constexpr (HELD::kCodes) return (uint64_t)(uint32_t)page * c.page_16 + (uint64_t)row * c.row_16;
+    else return ((uint64_t)(uint32_t)page * c.page_16 + (uint64_t)row * c.row_16) << 4;
   };
   auto load_tile = [&](int kb) {
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
       const uint64_t off = place_of(i, kb);
-      if (!S::kDirect) __builtin_memcpy(&kr[i], __builtin_assume_aligned(kp + (off << 4), sizeof(Load)), sizeof(Load));
-      __builtin_memcpy(&vr[i], __builtin_assume_aligned(vp + (off << 4), sizeof(Load)), sizeof(Load));
-      if constexpr (HELD::kCodes) {
+      if constexpr (!HELD::kCodes) {
+        kr[i] = *reinterpret_cast<const u32x4*>(kp + off);
+        vr[i] = *reinterpret_cast<const u32x4*>(vp + off);
+      } else {
+        if (!S::kDirect) __builtin_memcpy(&kr[i], __builtin_assume_aligned(kp + (off << 4), sizeof(Load)), sizeof(Load));
+        __builtin_memcpy(&vr[i], __builtin_assume_aligned(vp + (off << 4), sizeof(Load)), sizeof(Load));
         if (!S::kDirect) ke[i] = ks[off];
         ve[i] = vs[off];
       }
@@ -396,11 +405,10 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   const unsigned char* q_at =
       static_cast<const unsigned char*>(a.q) + ((long)(tok0 + my_tok) * a.q_ld + (long)qh * c.d) * S::kEsz;
   // (a lane group's pieces of a row: every kGroups-th, or where keys come as codes one run of them)
-  auto piece_of = [&](int s) { return S::kDirect ? grp * kSteps + s : M::kGroups * s + grp; };
   u32x4 q[kSteps];
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
-    const int e = piece_of(s) * M::kVec;
+    const int e = (S::kDirect ? grp * kSteps + s : M::kGroups * s + grp) * M::kVec;
     u32x4 v = *reinterpret_cast<const u32x4*>(q_at + (e < c.d ? e : 0) * S::kEsz);
     // (scale 0: queries of zeros, so that a hidden score stays -infinity)
     v = e < c.d && a.scale != 0.f ? v ^ flip : u32x4{0, 0, 0, 0};
@@ -411,28 +419,36 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   const int lim_last = row0 + wm * QW < rows ? __builtin_amdgcn_readlane(lim, 63) : -1;   // (none: no key)
   const int lim_block = causal ? min(kv - n + token_in(a, row0), last_key) : last_key;    // of the block's
 
-  // Load i of a thread to its 16-byte pieces of a tile's row.
-  auto store_row = [&](unsigned char* to, int i, const Load& x, uint32_t scale, bool on) {
-    constexpr int kSplit = S::kUnit / M::kVec;
-    const int row = my_row + i * S::kApart;
+  // (codes) load i of a thread to its 16-byte pieces of a tile's row
+  auto store_codes = [&](unsigned char* to, int i, const Load& x, uint32_t scale, bool on) {
+    if constexpr (HELD::kCodes) {
+      constexpr int kSplit = S::kUnit / M::kVec;
+      const int row = my_row + i * S::kApart;
 #pragma unroll
-    for (int j = 0; j < kSplit; ++j) {
-      u32x4 v;
-      if constexpr (HELD::kCodes) v = HELD::template piece<DT>(x.v[j * M::kVec / 8], scale, j * M::kVec / 4 % 2);
-      else v = x;
-      *reinterpret_cast<u32x4*>(to + row * RB + (((my_piece * kSplit + j) ^ mix<RB>(row)) << 4)) = on ? v : u32x4{0, 0, 0, 0};
+      for (int j = 0; j < kSplit; ++j) {
+        const u32x4 v = HELD::template piece<DT>(x.v[j * M::kVec / 8], scale, j * M::kVec / 4 % 2);
+        *reinterpret_cast<u32x4*>(to + row * RB + (((my_piece * kSplit + j) ^ mix<RB>(row)) << 4)) = on ? v : u32x4{0, 0, 0, 0};
+      }
     }
   };
   auto store_keys = [&](unsigned char* to) {
 #pragma unroll
-    for (int i = 0; i < S::kLoads; ++i) store_row(to, i, kr[i], ke[i], my_on);
+    for (int i = 0; i < S::kLoads; ++i) {
+      const int row = my_row + i * S::kApart;
+      if constexpr (HELD::kCodes) store_codes(to, i, kr[i], ke[i], my_on);
+      else *reinterpret_cast<u32x4*>(to + row * RB + ((my_piece ^ mix<RB>(row)) << 4)) = my_on ? kr[i] : u32x4{0, 0, 0, 0};
+    }
   };
   auto store_values = [&](unsigned char* to, int kb) {
     if (kb + KT > k1) {
       // What lies behind the keys may be anything; its weight is 0, and 0 times NaN is NaN.
 #pragma unroll
       for (int i = 0; i < S::kLoads; ++i)
-        if (kb + my_row + i * S::kApart >= k1) vr[i] = Load{}, ve[i] = 0;
+        if (kb + my_row + i * S::kApart >= k1) vr[i] = Load{};
+      if constexpr (HELD::kCodes) {
+#pragma unroll
+        for (int i = 0; i < S::kLoads; ++i) ve[i] = kb + my_row + i * S::kApart >= k1 ? 0 : ve[i];
+      }
     }
     if (kb + KT - 1 > lim_block && causal) {
       // Some row does not see some of these keys.  Their weight is 0 there, but its product with a value
@@ -449,7 +465,11 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
       if (odd) sh.odd_values[wk] = 1;
     }
 #pragma unroll
-    for (int i = 0; i < S::kLoads; ++i) store_row(to, i, vr[i], ve[i], true);
+    for (int i = 0; i < S::kLoads; ++i) {
+      const int row = my_row + i * S::kApart;
+      if constexpr (HELD::kCodes) store_codes(to, i, vr[i], ve[i], true);
+      else *reinterpret_cast<u32x4*>(to + row * RB + ((my_piece ^ mix<RB>(row)) << 4)) = vr[i];
+    }
   };
 
   // This lane's share of its query's result, four elements of the head at a time: quad number x is elements
@@ -634,7 +654,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
       for (int t = 0; t < kTiles; ++t) {
         __builtin_memcpy(&kc[t], __builtin_assume_aligned(static_cast<const unsigned char*>(a.k_pool) + (unit[t] << 4) + k_bytes, sizeof(Direct)),
                          sizeof(Direct));
-        kx[t] = (a.k_scales + unit[t])[k_units];
+        kx[t] = (scales.k + unit[t])[k_units];
       }
     };
     auto load_values = [&]() {
@@ -642,7 +662,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
       for (int t = 0; t < kTiles; ++t) {
         __builtin_memcpy(&vc[t], __builtin_assume_aligned(static_cast<const unsigned char*>(a.v_pool) + (unit[t] << 4) + v_bytes, sizeof(Direct)),
                          sizeof(Direct));
-        vx[t] = (a.v_scales + unit[t])[v_units];
+        vx[t] = (scales.v + unit[t])[v_units];
       }
     };
     if (mine > 0) {
@@ -763,10 +783,10 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
         float w = 0.f;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-          const int e = piece_of(s) * M::kVec;
+          const int e = (S::kDirect ? grp * kSteps + s : M::kGroups * s + grp) * M::kVec;
           Piece<DT, M::kVec> kf = {}, qf;
           if (e < c.d) {
-            if constexpr (HELD::kCodes) kf = HELD::template values<DT, M::kVec>(a.k_pool, a.k_scales, at + e);
+            if constexpr (HELD::kCodes) kf = HELD::template values<DT, M::kVec>(a.k_pool, scales.k, at + e);
             else kf = load_piece<DT, M::kVec>(a.k_pool, at + e);
           }
           __builtin_memcpy(&qf, &q[s], 16);
@@ -780,7 +800,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
         for (int x = 0; x < kQuads; ++x) {
           const long from = at + min(quad_at(x), c.d - 4);  // (past the head: not stored)
           Piece<DT, 4> v;
-          if constexpr (HELD::kCodes) v = HELD::template values<DT, 4>(a.v_pool, a.v_scales, from);
+          if constexpr (HELD::kCodes) v = HELD::template values<DT, 4>(a.v_pool, scales.v, from);
           else v = load_piece<DT, 4>(a.v_pool, from);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -902,13 +922,13 @@ __global__ __launch_bounds__(256, DT == kBF16 && DP <= 128 ? 2 : 1) void k_atten
 // the other; with many rows by memory (42 000 rows of two parts 15 us, of which a copy would need 11 for their 55 MB).  Two
 // parts are asked for at once: eight, of which those past the last are read in vain, take 2 us more there and gain nothing
 // with 63 parts.
-template <int DT>
+template <int DT, bool SHARED>
 __global__ __launch_bounds__(256) void k_attend_join(Attend a, Cache c, int pre_chunk, int pre_parts, int own_least, int own_share, const float* part_o,
                                                      const float2* part_ml, int lanes_shift, int split_shift) {
   __shared__ f32x4v set_x[256];
   __shared__ float2 set_ml[256];
   const int all = c.T * c.Hq;  // (2^24 at most)
-  const int own_chunk = part_keys(c, own_least, own_share);
+  const int own_chunk = SHARED ? part_keys(c, own_least, own_share) : own_least;
   const int lane = threadIdx.x & 63, set = threadIdx.x >> lanes_shift, sub = set & ((1 << split_shift) - 1);
   const int rows_shift = 8 - lanes_shift - split_shift;  // rows of a block
   const int first = (int)blockIdx.x << rows_shift, id = first + (set >> split_shift);

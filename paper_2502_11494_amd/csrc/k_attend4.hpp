@@ -8,7 +8,7 @@ namespace dart {
 
 // The tiles of attention over rows, keys and values brought to the rows' type on their way to LDS.
 template <int DT, int DP, int QW, int WM, int WK, int KT, class HELD>
-__global__ __launch_bounds__(64 * WM * WK, HELD::kPages && DT == kBF16 ? 3 : DP <= 128 && (DT == kBF16 || WK == 1) ? 2 : 1) void k_attend_4bit(Attend a, Cache c, Parting sp) {
+__global__ __launch_bounds__(64 * WM * WK, HELD::kPages && DT == kBF16 ? 3 : DP <= 128 && (DT == kBF16 || WK == 1) ? 2 : 1) void k_attend_4bit(Attend a, Scales scales, Cache c, Parting sp) {
   extern __shared__ __align__(16) unsigned char lds[];
   __shared__ AttendShared sh;
   long slot;
@@ -20,12 +20,12 @@ __global__ __launch_bounds__(64 * WM * WK, HELD::kPages && DT == kBF16 ? 3 : DP 
     head = (int)(rest % (unsigned)c.Hkv);
     slot = (long)(rest / (unsigned)c.Hkv);
   }
-  attend_tile<DT, DP, QW, WM, WK, KT, HELD>(a, c, sp, lds, sh, slot, head, part);
+  attend_tile<DT, DP, QW, WM, WK, KT, HELD>(a, c, sp, lds, sh, slot, head, part, scales);
 }
 
 // Prefixes and own keys in one launch.
 template <int DT, int DP, int KT>
-__global__ __launch_bounds__(256, DT == kBF16 && DP <= 128 ? 2 : 1) void k_attend_4bit_both(Attend a, Cache c, Parting pre, Parting own,
+__global__ __launch_bounds__(256, DT == kBF16 && DP <= 128 ? 2 : 1) void k_attend_4bit_both(Attend a, Scales scales, Cache c, Parting pre, Parting own,
                                                                                             unsigned pre_blocks) {
   extern __shared__ __align__(16) unsigned char lds[];
   __shared__ AttendShared sh;
@@ -34,8 +34,8 @@ __global__ __launch_bounds__(256, DT == kBF16 && DP <= 128 ? 2 : 1) void k_atten
   long slot;
   int head, part;
   attend_place(c, sp, first ? blockIdx.x : blockIdx.x - pre_blocks, slot, head, part);
-  if (sp.few) attend_tile<DT, DP, 16, 1, 4, 32, In4Bits>(a, c, sp, lds, sh, slot, head, part);
-  else attend_tile<DT, DP, many_columns(DT, DP), 4, 1, KT, In4Bits>(a, c, sp, lds, sh, slot, head, part);
+  if (sp.few) attend_tile<DT, DP, 16, 1, 4, 32, In4Bits>(a, c, sp, lds, sh, slot, head, part, scales);
+  else attend_tile<DT, DP, many_columns(DT, DP), 4, 1, KT, In4Bits>(a, c, sp, lds, sh, slot, head, part, scales);
 }
 
 }  // namespace dart
