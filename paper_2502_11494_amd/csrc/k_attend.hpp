@@ -1091,9 +1091,13 @@ inline Kind plan_parting(const Cache& c, int dtype, bool prefix, long rows, int 
   // 1024; 64 answers over one prefix of 9216 229, 43, 34, 42 and 48.  32-bit tiles of four waves are bound by the
   // matrix cores' latency and want company: 637 causal tokens of 32 heads 69 us in 320 blocks, 58 in 960.
   // Keys held in 4 bits are a quarter of the bytes, and single tokens need two blocks to a unit to have them come as fast: 32 tokens over
-  // 8704 keys each, 28 + 4 heads, 45 us with 256 blocks, 36 with 512, 42 with 1024; 64 over 4352 41, 35 and 43.
-  const long want = std::max(1L, (dtype == DART_F32 && kind == kMany ? 1024 : codes && kind == kFew ? 512 : 256) / blocks);
-  const long chunk = std::max(256L, ((max_keys + want - 1) / want + 255) / 256 * 256);
+  // 8704 keys each, 28 + 4 heads, 45 us with 256 blocks, 36 with 512, 42 with 1024; 64 over 4352 41, 35 and 43.  Beside the blocks of a
+  // prefix one is enough: four answers over 8000 keys of their own and a prefix of 9216 24 us with two, 19 with one.
+  // Tiles of many rows over them divide the keys to 64: 64 tokens over 9216 keys in 256 blocks 28 us, in 192 (parts to 256) 32; 64
+  // answers over that prefix 31 and 34.  Keys dealt to four waves come in steps of 256.
+  const long want = std::max(1L, (dtype == DART_F32 && kind == kMany ? 1024 : codes && kind == kFew && c.groups == 0 ? 512 : 256) / blocks);
+  const long unit = codes && kind != kFew ? 64 : 256;
+  const long chunk = std::max(256L, ((max_keys + want - 1) / want + unit - 1) / unit * unit);
   p.chunk = (int)chunk;
   p.chunks = std::max(1, (int)((max_keys + chunk - 1) / chunk));
   return kind;
