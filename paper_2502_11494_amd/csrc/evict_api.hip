@@ -22,12 +22,15 @@ struct GatherPlan {
   size_t total;
 };
 
-int keys_of_tile(int dtype, int d, bool few) { return few || (dtype == DART_BF16 && d <= 128) ? 256 : 128; }
+int keys_of_tile(int dtype, int d, bool few, bool codes) {
+  if (few) return 64 * few_tiles(dtype == DART_BF16 ? kBF16 : kF32, d, codes);
+  return dtype == DART_BF16 && d <= 128 ? 256 : 128;
+}
 
 // rows: (token, head) pairs of a sequence at most, of a group on average.
-dart_status plan_shares(const Cache& c, int dtype, long rows, long owners, int max_keys, Shares& s, size_t& bytes) {
+dart_status plan_shares(const Cache& c, int dtype, bool codes, long rows, long owners, int max_keys, Shares& s, size_t& bytes) {
   s.few = rows <= 48;
-  const int keys = keys_of_tile(dtype, c.d, s.few);
+  const int keys = keys_of_tile(dtype, c.d, s.few, codes);
   s.tiles = std::max(1, (int)(((long)max_keys + keys - 1) / keys));
   if (owners * s.tiles > kMaxTiles / c.Hkv) return DART_ERR_SHAPE;
   const long blocks = owners * s.tiles * c.Hkv, row_tiles = (rows + 31) / 32;
@@ -39,16 +42,16 @@ dart_status plan_shares(const Cache& c, int dtype, long rows, long owners, int m
   return DART_OK;
 }
 
-dart_status plan_gather(const Cache& c, int dtype, GatherPlan& p) {
+dart_status plan_gather(const Cache& c, int dtype, bool codes, GatherPlan& p) {
   const long r = c.Hq / c.Hkv;
   if (c.T * r > kMaxRows) return DART_ERR_SHAPE;
   p = {};
   size_t bytes = 0;
-  DART_TRY(plan_shares(c, dtype, c.max_q * r, std::max(c.B, 1), c.max_kv, p.own, bytes));
+  DART_TRY(plan_shares(c, dtype, codes, c.max_q * r, std::max(c.B, 1), c.max_kv, p.own, bytes));
   if (c.groups > 0) {
     p.pre.prefix = 1;
     const long rows = std::min((long)c.T, (long)c.max_q * c.B) * r;
-    DART_TRY(plan_shares(c, dtype, (rows + c.groups - 1) / c.groups, c.groups, c.max_prefix, p.pre, bytes));
+    DART_TRY(plan_shares(c, dtype, codes, (rows + c.groups - 1) / c.groups, c.groups, c.max_prefix, p.pre, bytes));
   }
   p.total = kAlign + (bytes + kAlign - 1) / kAlign * kAlign;
   return DART_OK;
@@ -57,7 +60,7 @@ dart_status plan_gather(const Cache& c, int dtype, GatherPlan& p) {
 template <int DT, int DP, class HELD>
 dart_status launch_gather(const Gather& a, const Cache& c, const Shares& sp, hipStream_t st) {
   typedef GatherShape<DT, DP> S;
-  static_assert(GatherFewShape::kKeys == 256 && S::kKeys == (DT == kBF16 && DP <= 128 ? 256 : 128), "keys_of_tile");
+  static_assert(S::kKeys == (DT == kBF16 && DP <= 128 ? 256 : 128), "keys_of_tile");
   const long blocks = (sp.prefix ? c.groups : c.B) * (long)sp.tiles * c.Hkv;
   for (long first = 0; first < blocks * sp.parts; first += kMaxBlocks) {
     const unsigned n = (unsigned)std::min(kMaxBlocks, blocks * sp.parts - first);
@@ -125,7 +128,7 @@ extern "C" {
 size_t dart_attend_weights_workspace_bytes(const dart_cache* cache, int32_t four_bit) {
   Cache c;
   GatherPlan p;
-  if (make_cache(cache, c, four_bit ? 4 : 0) != DART_OK || plan_gather(c, cache->dtype, p) != DART_OK) return 0;
+  if (make_cache(cache, c, four_bit ? 4 : 0) != DART_OK || plan_gather(c, cache->dtype, four_bit != 0, p) != DART_OK) return 0;
   return p.total;
 }
 
@@ -140,7 +143,7 @@ dart_status dart_attend_weights(const dart_cache* cache, const void* q, int64_t 
   if (!k_pool || !lse || !weights) return DART_ERR_NULL;
   if (off16(k_pool)) return DART_ERR_ALIGN;
   GatherPlan p;
-  DART_TRY(plan_gather(c, cache->dtype, p));
+  DART_TRY(plan_gather(c, cache->dtype, k_scales != nullptr, p));
   if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < p.total) return DART_ERR_WORKSPACE;
   c.status = status;
   const Gather a = {q, k_pool, static_cast<const uint8_t*>(k_scales), lse, weights, q_ld, scale, carry, causal != 0, 1.0 / (c.Hq / c.Hkv)};

@@ -296,17 +296,33 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_gather_weights(Gathe
   }
 }
 
-// A few rows: a wave takes tiles of 16 keys against 16 rows at a time and leaves LDS alone.  All its keys are asked for at once, so
-// that a call of single tokens is bound by memory.  NT: tiles of a wave (32 tokens over 1024 to 16 384 keys
-// held in 4 bits 26.4 us, with eight 29).
+// Two numbers of every lane, added over pairs of lane groups LANES apart: the lower group gets the sum of the first numbers, the
+// upper that of the second ones.
+template <int LANES>
+__device__ __forceinline__ float pairs_sum(float x, float y) {
+  if constexpr (LANES == 16) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  } else {
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+}
+
+// A few rows: a wave takes tiles of 16 keys against 16 rows at a time and leaves LDS alone.  All its keys are asked for at once, the rows
+// before them, so that a call of single tokens is bound by memory and, over codes, by instructions.  NT: tiles of a wave (32 tokens over
+// 8000 keys, 28 + 4 heads: in 4 bits 17.4 us with eight, 19.0 with four; in rows 54 with either, of 32 bits 212 and 111; with
+// 16 + 4 heads of 256 in 4 bits 36 and 33, of 32-bit queries 94 and 101).
+constexpr int few_tiles(int dt, int d, bool codes) { return codes && (dt == kF32 || d <= 128) ? 8 : 4; }
+template <int DT, int DP, bool CODES>
 struct GatherFewShape {
-  static constexpr int NT = 4;
+  static constexpr int NT = few_tiles(DT, DP, CODES);
   static constexpr int kKeys = 4 * 16 * NT;
 };
 
 template <int DT, int DP, class HELD>
 __global__ __launch_bounds__(256, DT == kF32 && DP == 256 ? 1 : 2) void k_gather_weights_few(Gather a, Cache c, Shares sp, unsigned first) {
-  typedef GatherFewShape S;
+  typedef GatherFewShape<DT, DP, HELD::kCodes> S;
   typedef Math<DT, 16> M;
   constexpr int NT = S::NT, kSteps = M::template steps<DP>(), kMine = DP / 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, grp = lane >> 4, col = lane & 15;
@@ -323,13 +339,27 @@ __global__ __launch_bounds__(256, DT == kF32 && DP == 256 ? 1 : 2) void k_gather
   const bool causal = a.causal && !sp.prefix;
   const int rows = s.n * r, row_first = causal ? max(0, k0 - s.fresh) * r : 0, mask = (1 << c.page_shift) - 1;
 
-  // ---- keys: of key `col` of a tile the lane group's pieces of the row, every fourth, or one run of codes
+  // ---- rows.  The first are asked for before the keys: after them they would come a look into memory later.
   auto piece = [&](int st) { return HELD::kCodes ? grp * kSteps + st : 4 * st + grp; };
+  float lse;
+  int lim;
+  u32x4 q[kSteps];
+  auto load_rows = [&](int row0) {
+    const int row = row0 + col, have = min(row, rows - 1), tok = (int)(((double)have + 0.5) * a.per_token), qh = head * r + have - tok * r;
+    lse = a.lse[(long)(s.tok0 + tok) * c.Hq + qh];
+    lim = row >= rows ? -1 : causal ? min(s.fresh + tok, last_key) : last_key;
+    const unsigned char* q_at = static_cast<const unsigned char*>(a.q) + ((long)(s.tok0 + tok) * a.q_ld + (long)qh * c.d) * (16 / M::kVec);
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st) q[st] = *reinterpret_cast<const u32x4*>(q_at + (piece(st) * M::kVec < c.d ? piece(st) * 16 : 0));
+  };
+  load_rows(row_first);
+
+  // ---- keys: of key `col` of a tile the lane group's pieces of the row, every fourth, or one run of codes
   int page[NT], page_out[NT / 4];
 #pragma unroll
   for (int t = 0; t < NT; ++t) page[t] = s.table[min(k0 + t * 16 + col, last_key) >> c.page_shift];
-  // (the keys that this lane writes: of tile 4 x + col / 4 key 4 grp + col % 4)
-  auto key_out = [&](int x) { return k0 + (4 * x + (col >> 2)) * 16 + 4 * grp + (col & 3); };
+  // (a lane writes key `col` of tile 4 x + grp)
+  auto key_out = [&](int x) { return k0 + (4 * x + grp) * 16 + col; };
 #pragma unroll
   for (int x = 0; x < NT / 4; ++x) page_out[x] = s.table[min(key_out(x), last_key) >> c.page_shift];
   bool bad = false;
@@ -360,34 +390,35 @@ __global__ __launch_bounds__(256, DT == kF32 && DP == 256 ? 1 : 2) void k_gather
     }
   }
   if (bad) flag(c, kBadPage);
+  // What the keys had, asked for beside their codes (of a key that is not there, some place's; a branch would wait for it).
   float old[NT / 4];
   float* put[NT / 4];
+  bool keeps[NT / 4], there[NT / 4];
 #pragma unroll
   for (int x = 0; x < NT / 4; ++x) {
-    const bool none = (unsigned)page_out[x] >= (unsigned)c.n_pages || key_out(x) > last_key;
-    put[x] = none ? nullptr : a.weights + (((long)page_out[x] * c.Hkv + head) << c.page_shift) + (key_out(x) & mask);
-    old[x] = a.carry == 0.f || none || key_out(x) >= s.fresh ? 0.f : a.carry * *put[x];
+    const int key = key_out(x);
+    const bool none = (unsigned)page_out[x] >= (unsigned)c.n_pages;
+    there[x] = !none && key <= last_key;
+    keeps[x] = key < s.fresh;
+    put[x] = a.weights + (((none ? 0L : (long)page_out[x]) * c.Hkv + head) << c.page_shift) + (key & mask);
+    old[x] = 0.f;
+    if (a.carry != 0.f) old[x] = *put[x];
   }
 
   const float scale2 = a.scale * kLog2e;
-  float sum[NT][4];
+  float sum[NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int u = 0; u < 4; ++u) sum[t][u] = 0.f;
+  for (int t = 0; t < NT; ++t) sum[t] = 0.f;
   for (int row0 = row_first; row0 < rows; row0 += 16) {
-    const int row = row0 + col, have = min(row, rows - 1), tok = (int)(((double)have + 0.5) * a.per_token), qh = head * r + have - tok * r;
-    const float lse = a.lse[(long)(s.tok0 + tok) * c.Hq + qh];
-    const int lim = row >= rows || lse == -INFINITY ? -1 : causal ? min(s.fresh + tok, last_key) : last_key;
-    const unsigned char* q_at = static_cast<const unsigned char*>(a.q) + ((long)(s.tok0 + tok) * a.q_ld + (long)qh * c.d) * (16 / M::kVec);
-    u32x4 q[kSteps];
+    if (row0 > row_first) load_rows(row0);
+    // (keys lie in the columns of the product, this lane group's four rows in its registers)
+    float less[4];
+    int lims[4];
 #pragma unroll
-    for (int st = 0; st < kSteps; ++st) {
-      const int e = piece(st) * M::kVec;
-      q[st] = u32x4{0, 0, 0, 0};
-      if (e < c.d && a.scale != 0.f) q[st] = *reinterpret_cast<const u32x4*>(q_at + e * (16 / M::kVec));
-    }
-    const float lse2 = lse * kLog2e;
+    for (int u = 0; u < 4; ++u) less[u] = __shfl(lse * kLog2e, 4 * grp + u), lims[u] = __shfl(lse == -INFINITY ? -1 : lim, 4 * grp + u);
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st)
+      if (piece(st) * M::kVec >= c.d || a.scale == 0.f) q[st] = u32x4{0, 0, 0, 0};
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       if constexpr (HELD::kCodes) {
@@ -404,33 +435,20 @@ __global__ __launch_bounds__(256, DT == kF32 && DP == 256 ? 1 : 2) void k_gather
         } else {
           k = kr[t][st];
         }
-        x = M::qk(k, q[st], x);
+        x = M::qk(q[st], k, x);
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const float y = __builtin_amdgcn_exp2f(fmaf(x[u], scale2, -lse2));
-        sum[t][u] += k0 + t * 16 + 4 * grp + u <= lim ? y : 0.f;
+        const float y = __builtin_amdgcn_exp2f(fmaf(x[u], scale2, -less[u]));
+        sum[t] += k0 + t * 16 + col <= lims[u] ? y : 0.f;
       }
     }
   }
-  // ---- over the 16 columns, by rotations of them; then every lane has the four sums of each tile
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      float y = sum[t][u];
-      y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x128, 0xf, 0xf, true));
-      y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x124, 0xf, 0xf, true));
-      y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x122, 0xf, 0xf, true));
-      y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x121, 0xf, 0xf, true));
-      sum[t][u] = y;
-    }
+  // ---- over the lane groups; each then has the sums of a tile of its own
 #pragma unroll
   for (int x = 0; x < NT / 4; ++x) {
-    float mine = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) mine = col == i ? sum[4 * x + i / 4][i % 4] : mine;
-    if (put[x] != nullptr) *put[x] = mine + old[x];
+    const float mine = pairs_sum<16>(pairs_sum<32>(sum[4 * x], sum[4 * x + 2]), pairs_sum<32>(sum[4 * x + 1], sum[4 * x + 3]));
+    if (there[x]) *put[x] = keeps[x] && a.carry != 0.f ? fmaf(a.carry, old[x], mine) : mine;
   }
 }
 

@@ -17,6 +17,8 @@ T __shfl_up(T v, int by) {
   const int l = lane_now & 63;
   return from_lane(v, l >= by ? l - by : l);
 }
+template <class T>
+T __shfl(T v, int lane) { return from_lane(v, lane & 63); }
 inline int __popcll(unsigned long long x) { return __builtin_popcountll(x); }
 inline int atomicAdd(int* p, int v) {
   const int old = *p;
