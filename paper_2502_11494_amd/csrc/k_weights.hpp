@@ -85,11 +85,20 @@ __device__ __forceinline__ Share share_of(const Cache& c, bool prefix, int owner
   return s;
 }
 
+// A key's weight; of one in a page that is none (flagged where its key was asked for) another's, not to be written.
+__device__ __forceinline__ float* weight_at(const Gather& a, const Cache& c, int head, int key, int page) {
+  const bool none = (unsigned)page >= (unsigned)c.n_pages;
+  return a.weights + (((none ? 0L : (long)page) * c.Hkv + head) << c.page_shift) + (key & ((1 << c.page_shift) - 1));
+}
+__device__ __forceinline__ float kept_weight(const Gather& a, const Share& s, int key, float old, float sum) {
+  return a.carry == 0.f || key >= s.fresh ? sum : fmaf(a.carry, old, sum);
+}
+
 __device__ __forceinline__ void put_weight(const Gather& a, const Cache& c, const Share& s, int head, int key, float sum) {
   const int page = s.table[key >> c.page_shift];
-  if ((unsigned)page >= (unsigned)c.n_pages) return;  // (flagged where its key was asked for)
-  float* at = a.weights + (((long)page * c.Hkv + head) << c.page_shift) + (key & ((1 << c.page_shift) - 1));
-  *at = a.carry == 0.f || key >= s.fresh ? sum : fmaf(a.carry, *at, sum);
+  if ((unsigned)page >= (unsigned)c.n_pages) return;
+  float* at = weight_at(a, c, head, key, page);
+  *at = kept_weight(a, s, key, a.carry != 0.f ? *at : 0.f, sum);
 }
 
 // w_j <- carry * w_j + sum over the rows that see key j of exp(scale <q, k_j> - lse).  A wave holds its keys in registers
@@ -393,14 +402,12 @@ __global__ __launch_bounds__(256, DT == kF32 && DP == 256 ? 1 : 2) void k_gather
   // What the keys had, asked for beside their codes (of a key that is not there, some place's; a branch would wait for it).
   float old[NT / 4];
   float* put[NT / 4];
-  bool keeps[NT / 4], there[NT / 4];
+  bool there[NT / 4];
 #pragma unroll
   for (int x = 0; x < NT / 4; ++x) {
     const int key = key_out(x);
-    const bool none = (unsigned)page_out[x] >= (unsigned)c.n_pages;
-    there[x] = !none && key <= last_key;
-    keeps[x] = key < s.fresh;
-    put[x] = a.weights + (((none ? 0L : (long)page_out[x]) * c.Hkv + head) << c.page_shift) + (key & mask);
+    there[x] = (unsigned)page_out[x] < (unsigned)c.n_pages && key <= last_key;
+    put[x] = weight_at(a, c, head, key, page_out[x]);
     old[x] = 0.f;
     if (a.carry != 0.f) old[x] = *put[x];
   }
@@ -448,7 +455,7 @@ __global__ __launch_bounds__(256, DT == kF32 && DP == 256 ? 1 : 2) void k_gather
 #pragma unroll
   for (int x = 0; x < NT / 4; ++x) {
     const float mine = pairs_sum<16>(pairs_sum<32>(sum[4 * x], sum[4 * x + 2]), pairs_sum<32>(sum[4 * x + 1], sum[4 * x + 3]));
-    if (there[x]) *put[x] = keeps[x] && a.carry != 0.f ? fmaf(a.carry, old[x], mine) : mine;
+    if (there[x]) *put[x] = kept_weight(a, s, key_out(x), old[x], mine);
   }
 }
 
@@ -462,9 +469,21 @@ __global__ __launch_bounds__(256) void k_join_weights(Gather a, Cache c, Shares 
   const int key = tile * keys + (int)threadIdx.x;
   if (!s.valid || s.n <= 0 || key >= s.kv || (int)threadIdx.x >= keys) return;
   const long blocks = (long)(sp.prefix ? c.groups : c.B) * sp.tiles * c.Hkv;
-  float sum = 0.f;
-  for (int p = 0; p < sp.parts; ++p) sum += sp.sums[(p * blocks + blockIdx.x) * keys + threadIdx.x];
-  put_weight(a, c, s, head, key, sum);
+  const int page = s.table[key >> c.page_shift];
+  float sum = 0.f, old = 0.f;
+  float* at = nullptr;
+  for (int p0 = 0; p0 < sp.parts; p0 += 8) {  // (eight on their way together: 637 causal tokens of 32 heads in 32 bits 33.2 us, one by one 34.2)
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = sp.sums[(min(p0 + i, sp.parts - 1) * blocks + blockIdx.x) * keys + threadIdx.x];
+    if (p0 == 0) {
+      at = weight_at(a, c, head, key, page);
+      if (a.carry != 0.f) old = *at;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += p0 + i < sp.parts ? v[i] : 0.f;
+  }
+  if ((unsigned)page < (unsigned)c.n_pages) *at = kept_weight(a, s, key, old, sum);
 }
 
 }  // namespace dart
