@@ -77,18 +77,22 @@ __global__ __launch_bounds__(W * kWave) void k_evict_select(Evict a, Cache c) {
     }
     if (!valid) continue;
     int* kept = a.kept + id * a.kept_ld;
+    const int* table = c.pages + (long)b * c.pages_ld;
+    // The pages of all keys, by the first head's block for all heads: the choice looks at some keys only, the move at those kept.
+    bool missing = false;
+    if (h == 0)
+      for (int p = tid; p <= (kv - 1) >> c.page_shift; p += kThreads) missing |= (unsigned)table[p] >= (unsigned)c.n_pages;
     if (keep == kv) {
+      if (missing) flag(c, kBadPage);
       for (int j = tid; j < kv; j += kThreads) kept[j] = j;
       continue;
     }
-    const int* table = c.pages + (long)b * c.pages_ld;
     // candidates first .. first + n - 1, of which `want` are taken
     const int n = kv - a.recent - a.first, want = keep - a.recent - a.first;
     for (int j = tid; j < a.first; j += kThreads) kept[j] = j;
     for (int j = tid; j < a.recent; j += kThreads) kept[a.first + want + j] = kv - a.recent + j;
     const int groups = (n + kHeld - 1) / kHeld;
     uint32_t u[H];
-    bool bad = false;
     auto place = [&](int g, int i) { return g * kHeld + (wave * H + i) * kWave + lane; };
     auto load = [&](int g) {
       int page[H];
@@ -100,7 +104,6 @@ __global__ __launch_bounds__(W * kWave) void k_evict_select(Evict a, Cache c) {
         const int row = (a.first + min(place(g, i), n - 1)) & ((1 << c.page_shift) - 1);
         const float w = a.weights[(((long)(none ? 0 : page[i]) * c.Hkv + h) << c.page_shift) + row];
         u[i] = none ? 0u : order_of(w);
-        bad = bad || none;
       }
     };
 
@@ -125,7 +128,7 @@ __global__ __launch_bounds__(W * kWave) void k_evict_select(Evict a, Cache c) {
       lo = sh.low[w] < lo ? sh.low[w] : lo;
       hi = sh.high[w] > hi ? sh.high[w] : hi;
     }
-    if (bad) sh.bad = 1;
+    if (missing) sh.bad = 1;
 
     // ---- the border: [lo, lo + 2^bits) holds it; `need` of the weights in it are taken, all above are
     int bits = hi == lo ? 0 : 32 - __builtin_clz(hi - lo), need = want, inside = n;
