@@ -501,7 +501,8 @@ DART_API dart_status dart_attend(const dart_cache* cache, const void* q, int64_t
  * 0, 0.5, 1, 1.5, 2, 3, 4, 6 (bits 0-2: 0..7); the value is their product, which bfloat16 and 32 bits hold exactly.
  * e is the smallest from 0 to 252 that leaves the block's largest value under 7 * 2^(e - 127) (252: whatever it is), and a
  * value becomes the nearest of the 15, a tie the even code, the largest where it lies beyond.  A block with an infinity or
- * NaN has e = 255 and is read as NaN throughout.
+ * NaN has e = 255 and is read as NaN throughout.  No call writes 253 or 254; they are read as their products, infinities where
+ * those pass the type's range.
  * A pool is two arrays: `codes` (16-byte aligned) and `scales`.  With W = d rounded up to 32, the strides page_ld, head_ld and
  * row_ld of its dart_cache count values and are multiples of 32, W <= row_ld: key head h of row r of page p has value i at bit
  * 4 * (x + i) of codes, x = p*page_ld + h*head_ld + r*row_ld (the even value of a byte in its low half), and the

@@ -33,7 +33,9 @@ struct In4Bits {
   static constexpr bool kCodes = true, kPages = false;
   // Values of a load, where a thread has a share of them: 32 (a block), 16 or 8.
   static constexpr int unit(int, int share) { return share < kBlock ? share : kBlock; }
-  __device__ static __forceinline__ bool no_number(uint32_t scale) { return scale == kNoNumber; }
+  // Whether a block may hold infinities or NaN: 253 and 254, which no append writes, take the largest codes beyond 32 bits.
+  __device__ static __forceinline__ bool odd(uint32_t scale) { return scale > kTopScale; }
+  __device__ static __forceinline__ bool odd(const uint8_t* scales, long at) { return odd(scales[at / kBlock]); }
 
   // A 16-byte piece of a row: the eight bf16 values of a word of codes, or the half-th four of them in 32 bits.
   template <int DT>

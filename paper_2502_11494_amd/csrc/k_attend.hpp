@@ -457,7 +457,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
 #pragma unroll
       for (int i = 0; i < S::kLoads; ++i) {
         if constexpr (HELD::kCodes) {
-          if (HELD::no_number(ve[i])) vr[i] = Load{}, ve[i] = 0, odd = 1;
+          if (HELD::odd(ve[i])) vr[i] = Load{}, ve[i] = 0, odd = 1;
         } else {
           odd |= drop_infinities<DT>(vr[i]);
         }
@@ -700,10 +700,10 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
           if (kb + t * QW + v_row >= k1) vc[t] = Direct{}, vx[t] = 0;
       }
       if (kb + KT - 1 > lim_block && causal) {
-        // (values that are no numbers and that some row does not see: left out here and added at the end)
+        // (blocks that may hold values that are no numbers and that some row does not see: left out here and added at the end)
 #pragma unroll
         for (int t = 0; t < kTiles; ++t)
-          if (HELD::no_number(vx[t])) vc[t] = Direct{}, vx[t] = 0, sh.odd_values[wk] = 1;
+          if (HELD::odd(vx[t])) vc[t] = Direct{}, vx[t] = 0, sh.odd_values[wk] = 1;
       }
 #pragma unroll
       for (int sub = 0; sub < kSub; ++sub) {
@@ -773,7 +773,7 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
   if (causal) {
     if (WM > 1) __syncthreads();
     if (*(volatile int*)&sh.odd_values[wk] != 0) {
-      // Values that are no numbers, key by key, for the rows that see them.
+      // Values that are no numbers, and blocks of codes that may hold such, key by key, for the rows that see them.
 #pragma unroll 1
       for (int it = 0; it < steps * KT; ++it) {
         const int kb = kfirst + it / KT * kstep, key = kb + it % KT;
@@ -800,11 +800,17 @@ __device__ __forceinline__ void attend_tile(const Attend& a, const Cache& c, con
         for (int x = 0; x < kQuads; ++x) {
           const long from = at + min(quad_at(x), c.d - 4);  // (past the head: not stored)
           Piece<DT, 4> v;
-          if constexpr (HELD::kCodes) v = HELD::template values<DT, 4>(a.v_pool, scales.v, from);
-          else v = load_piece<DT, 4>(a.v_pool, from);
+          bool all = false;  // (of codes the whole block was left out)
+          if constexpr (HELD::kCodes) {
+            all = HELD::odd(scales.v, from);
+            if (!all) continue;
+            v = HELD::template values<DT, 4>(a.v_pool, scales.v, from);
+          } else {
+            v = load_piece<DT, 4>(a.v_pool, from);
+          }
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            if (fabsf(v.get(k)) < INFINITY) continue;
+            if (!all && fabsf(v.get(k)) < INFINITY) continue;
             if constexpr (DT == kBF16) o[x / (M::kRegs / 4)][4 * (x % (M::kRegs / 4)) + k] += w * v.get(k);
             else o[4 * (x / M::kRegs) + k][x % M::kRegs] += w * v.get(k);
           }

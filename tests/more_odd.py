@@ -39,3 +39,48 @@ def bad_pages_of_evicted_keys(evict):
             table[0, 7:] = -3  # behind the keys: not looked at
             table[2, 6:] = 1 << 30
             assert evict(c, w, table=table, **how)[4] == 0
+
+
+def put_block(pool, page, head, row, block, scale, codes):
+    """Scale and 32 codes of one block of a pool."""
+    pool[1][page, head, row, block] = scale
+    pool[0][page, head, row, 16 * block:16 * block + 16] = codes[::2] + 16 * codes[1::2]
+
+
+def scales_that_no_append_writes_read(read):
+    """Scale bytes 253 and 254 are read as their products, which the largest codes take beyond the type."""
+    for dtype in ("bf16", "f32"):
+        c = U.make([3], [3], 1, 1, 32, 16, dtype, seed=1)
+        page, row = U.places(c, 0)
+        codes = torch.arange(32, dtype=torch.uint8) % 16
+        for t, scale in enumerate((252, 253, 254)):
+            for pool in c.four:
+                put_block(pool, page[t], 0, row[t], 0, scale, codes)
+        want = torch.stack([U.GRID[codes.long() & 7] * torch.where(codes > 7, -1.0, 1.0) * 2.0 ** (e - 127) for e in (252, 253, 254)])
+        for got in read(c)[:2]:
+            assert torch.equal(got, want.to(c.dtype))
+            assert torch.isinf(got.float()).sum(1).tolist() == [0, 8, 16]
+
+
+def scales_that_no_append_writes_attend(attend):
+    """Values of such a block, infinite and finite, go to the rows that see their key, and to no others."""
+    for dtype in ("bf16", "f32"):
+        # many rows; few, in pages that hold whole tiles and in smaller ones; wide heads
+        for n, d, page in (([70, 1], 96, 16), ([6], 96, 16), ([6], 96, 4), ([6], 256, 16), ([70], 256, 16)):
+            for scale in (253, 254):
+                c = U.make(n, [130, 40][:len(n)], 4, 2, d, page, dtype, seed=9)
+                at, row = U.places(c, 0)
+                key = 126  # seen by the last four tokens of the first sequence
+                # codes of 0, of 2^(scale - 128) and of what is infinite
+                codes = torch.tensor([0, 1, 9, 7], dtype=torch.uint8).repeat(8)
+                put_block(c.four[1], at[key], 1, row[key], 1, scale, codes)
+                c.v_pool[at[key], 1, row[key], 32:64] = torch.tensor([0.0, 0.5, -0.5, 0.0], dtype=torch.float64).repeat(8) * 2.0 ** (scale - 127)
+                # (scores so near one another that weights of the running reference do not carry the finite ones out of range)
+                want, want_lse, tol, lse_tol = A.reference(c, 0.02, True)
+                out, lse, status = attend(c, scale=0.02)[:3]
+                assert status == 0
+                spoilt = torch.zeros(out.shape, dtype=torch.bool)
+                spoilt[n[0] - 4:n[0], 2:, 35:64:4] = True
+                assert bool((out[spoilt] == float("inf")).all()), (dtype, n, d, page, scale)
+                assert bool(((out.double() - want).abs() <= tol)[~spoilt].all()), (dtype, n, d, page, scale)
+                assert bool(((lse.double() - want_lse).abs() <= lse_tol).all())

@@ -9,3 +9,8 @@ pytestmark = pytest.mark.gpu
 
 def test_bad_pages_of_evicted_keys():
     more_odd.bad_pages_of_evicted_keys(G.evict)
+
+
+def test_scales_that_no_append_writes():
+    more_odd.scales_that_no_append_writes_read(G.read)
+    more_odd.scales_that_no_append_writes_attend(G.attend)

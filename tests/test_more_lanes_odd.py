@@ -8,7 +8,8 @@ import pytest
 HERE = os.path.dirname(os.path.abspath(__file__))
 sys.path[:0] = [HERE, os.path.dirname(HERE)]
 
-CHECKS = {"bad_pages_of_evicted_keys": "evict"}
+CHECKS = {"bad_pages_of_evicted_keys": "evict", "scales_that_no_append_writes_read": "read",
+          "scales_that_no_append_writes_attend": "attend"}
 
 
 @pytest.mark.parametrize("check", sorted(CHECKS))
