@@ -84,3 +84,96 @@ def scales_that_no_append_writes_attend(attend):
                 assert bool((out[spoilt] == float("inf")).all()), (dtype, n, d, page, scale)
                 assert bool(((out.double() - want).abs() <= tol)[~spoilt].all()), (dtype, n, d, page, scale)
                 assert bool(((lse.double() - want_lse).abs() <= lse_tol).all())
+
+
+def many_rows(dtype, four, join=False, **more):
+    """A case whose rows gathered weights take by tiles of many (over 48 of a sequence); join: in several parts."""
+    n, kv = ([1, 300, 6], [50, 420, 6]) if join else ([1, 90, 6], [90, 150, 2])
+    return U.make(n, kv, 4, 2 if not join else 1, 64, 16, dtype, seed=6, four=four, **more)
+
+
+def old_weights(c):
+    return torch.rand((c.k_pool.shape[0], c.k_pool.shape[1], c.page), generator=torch.Generator().manual_seed(3))
+
+
+def weights_of_many_rows(weights):
+    """Scales of either sign and none, rows that see nothing, numbers that are none, skipped sequences: by the tiles of many rows,
+    in one part and in several."""
+    inf, nan = float("inf"), float("nan")
+    for dtype in ("bf16", "f32"):
+        for four in (False, True):
+            for join in (False, True):
+                where = (dtype, four, join)
+                c = many_rows(dtype, four, join)
+                old = old_weights(c)
+                for scale in (-0.3, 0.0, 1.0):
+                    for causal in (True, False):
+                        lse = A.reference(c, scale, causal)[1].float()
+                        got, status = weights(c, lse, old, scale=scale, causal=causal, carry=0.5)[:2]
+                        assert status == 0
+                        U.check_gathered(c, got, lse, old, scale=scale, causal=causal, carry=0.5)
+
+                # lse that is no number: -inf gives nothing, +inf neither, NaN goes to the keys that the row sees
+                scale = 0.1
+                lse = A.reference(c, scale, True)[1].float()
+                t, last = int(c.cu[1]) + 20, c.kv[1] - c.n[1] + 20  # a token of the second sequence, the last key it sees
+                good = weights(c, lse, old, scale=scale)[0]
+                one = lse.clone()
+                one[t, 1] = -inf
+                none = weights(c, one, old, scale=scale)[0]
+                U.check_gathered(c, none, one, old, scale=scale, causal=True, carry=1.0)
+                one[t, 1] = inf  # (exp(s - inf) = 0; no finite error can be derived from such an lse)
+                assert torch.equal(weights(c, one, old, scale=scale)[0], none), where
+                one[t, 1] = nan
+                got = weights(c, one, old, scale=scale)[0]
+                page, row = U.places(c, 1)
+                spoilt = torch.zeros(got.shape, dtype=torch.bool)
+                spoilt[page[:last + 1], 0, row[:last + 1]] = True
+                assert torch.isnan(got[spoilt]).all() and torch.equal(got[~spoilt], good[~spoilt]), where
+
+                # keys that are none spoil their own weight, whether all rows of a tile see them or some
+                d = many_rows(dtype, four, join)
+                spoilt = torch.zeros(got.shape, dtype=torch.bool)
+                for key in (5, c.kv[1] - c.n[1] + 70, c.kv[1] - 1):
+                    at = int(page[key]), 0, int(row[key])
+                    spoilt[at] = True
+                    if four:
+                        d.four[0][1][(*at, 1)] = 255
+                    else:
+                        d.k_pool[(*at, 33)] = nan
+                got = weights(d, lse, old, scale=scale)[0]
+                assert torch.isnan(got[spoilt]).all() and torch.equal(got[~spoilt], good[~spoilt]), where
+
+                # a sequence that is skipped keeps its weights, a key whose page is none has none; the others are as always
+                kv = torch.tensor(c.kv, dtype=torch.int32)
+                kv[1] = -4
+                got, status = weights(c, lse, old, scale=scale, kv=kv)[:2]
+                assert status == 1 and torch.equal(got[page, :, row], old[page, :, row])
+                for b in (0, 2):
+                    at, r = U.places(c, b)
+                    assert torch.equal(got[at, :, r], good[at, :, r]), where
+                table = c.table.clone()
+                table[1, 2] = 1 << 29
+                got, status = weights(c, lse, old, scale=scale, table=table)[:2]
+                keys = torch.arange(c.kv[1])
+                lost = (keys >= 32) & (keys < 48)
+                assert status == 2 and torch.equal(got[page[~lost], :, row[~lost]], good[page[~lost], :, row[~lost]]), where
+                assert torch.equal(got[page[lost], :, row[lost]], old[page[lost], :, row[lost]]), where
+
+
+def weights_of_prefixes_of_many_rows(weights):
+    """A group with a skipped sequence is skipped whole; the other one is as always."""
+    for dtype in ("bf16", "f32"):
+        for four in (False, True):
+            c = U.make([80, 3, 120], [85, 20, 130], 4, 2, 64, 16, dtype, groups=[2, 1], prefix=[200, 300], seed=6, four=four)
+            lse, old = A.reference(c, -0.1, True)[1].float(), old_weights(c)
+            good, status = weights(c, lse, old, scale=-0.1, carry=0.25)[:2]
+            assert status == 0
+            U.check_gathered(c, good, lse, old, scale=-0.1, causal=True, carry=0.25)
+            kv = torch.tensor(c.kv, dtype=torch.int32)
+            kv[1] = 1 << 20
+            got, status = weights(c, lse, old, scale=-0.1, carry=0.25, kv=kv)[:2]
+            assert status == 1
+            for places, same in ((U.places(c, 0), good), (U.places(c, 1), old), (U.places(c, 2), good),
+                                 (U.places(c, None, 200, c.front[0]), old), (U.places(c, None, 300, c.front[1]), good)):
+                assert torch.equal(got[places[0], :, places[1]], same[places[0], :, places[1]])

@@ -14,3 +14,8 @@ def test_bad_pages_of_evicted_keys():
 def test_scales_that_no_append_writes():
     more_odd.scales_that_no_append_writes_read(G.read)
     more_odd.scales_that_no_append_writes_attend(G.attend)
+
+
+def test_weights_of_many_rows():
+    more_odd.weights_of_many_rows(G.weights)
+    more_odd.weights_of_prefixes_of_many_rows(G.weights)

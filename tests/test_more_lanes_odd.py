@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 sys.path[:0] = [HERE, os.path.dirname(HERE)]
 
 CHECKS = {"bad_pages_of_evicted_keys": "evict", "scales_that_no_append_writes_read": "read",
-          "scales_that_no_append_writes_attend": "attend"}
+          "scales_that_no_append_writes_attend": "attend", "weights_of_many_rows": "weights",
+          "weights_of_prefixes_of_many_rows": "weights"}
 
 
 @pytest.mark.parametrize("check", sorted(CHECKS))
