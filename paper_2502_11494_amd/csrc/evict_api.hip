@@ -182,7 +182,7 @@ dart_status dart_evict(const dart_cache* cache, const dart_eviction* eviction, v
   if (kept && (kept_ld < p.most || kept_ld > (int64_t)1 << 33)) return DART_ERR_SHAPE;
   if (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0 || ws_bytes < p.total) return DART_ERR_WORKSPACE;
   c.status = status;
-  Evict a = {eviction->budget, eviction->ratio_num, std::max(eviction->ratio_den, 1), eviction->first, eviction->recent, p.most, weights,
+  Evict a = {eviction->budget, eviction->ratio_num, std::max(eviction->ratio_den, 1), eviction->first, eviction->recent, weights,
              weights_out, kept ? kept : static_cast<int*>(ws), kept ? (long)kept_ld : (long)p.most,
              reinterpret_cast<int2*>(static_cast<unsigned char*>(ws) + p.left), kv_len_out};
   const hipStream_t st = static_cast<hipStream_t>(stream);

@@ -7,7 +7,6 @@ namespace dart {
 
 struct Evict {
   int budget, num, den, first, recent;
-  int most;               // keys that any sequence keeps, at most
   const float* weights;
   float* weights_out;     // or nullptr
   int* kept;              // [B][Hkv], kept_ld apart
