@@ -58,7 +58,9 @@ __device__ __forceinline__ int lanes_sum(int x) {
 // are left, as whole numbers of their order, is cut in 2048 buckets, and the one that the border falls in is the next range,
 // until so few weights are left that each is compared with all others, or all that are left are alike.  Then the keys up to the
 // border are counted to their places in order.  A block of W waves, a wave H times 64 keys in a row; so many keys (H * W * 64)
-// are read once and held in registers, longer sequences are read again by every step.
+// are read once and held in registers, longer sequences are read again by every step.  Bound by latency, a few looks into memory and
+// LDS one after the other: 637 keys of 32 heads 7 us; 32 sequences of 1024 to 16 384 keys, 4 heads (128 blocks), 25 us, 5 each in the range,
+// two cuts and the places.
 template <int W, int H>
 __global__ __launch_bounds__(W * kWave) void k_evict_select(Evict a, Cache c) {
   __shared__ SelectShared<W> sh;
@@ -264,7 +266,9 @@ __global__ __launch_bounds__(W * kWave) void k_evict_select(Evict a, Cache c) {
 
 // Row i of a key head takes row kept[i] >= i.  A block has one column of one array of one key head of one sequence and goes through
 // its rows from the front, a chunk at a time: a chunk's rows are read, then written.  What it writes has been read, by itself or
-// before: row i is the source of no row after i.  So no copy of the rows is needed, and blocks do not wait for one another.
+// before: row i is the source of no row after i.  So no copy of the rows is needed, and blocks do not wait for one another.  Bound by
+// memory: 64 sequences of 2100 keys to 2048 in bf16 4.8 TB/s, choice included; those 32 to 11.1 %, 127 MB, 36 us, 27 where the call before
+// left some of the rows in the last cache.
 struct Column {
   unsigned char* from;
   unsigned char* to;

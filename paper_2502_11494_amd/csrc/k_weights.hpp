@@ -103,7 +103,10 @@ __device__ __forceinline__ void put_weight(const Gather& a, const Cache& c, cons
 
 // w_j <- carry * w_j + sum over the rows that see key j of exp(scale <q, k_j> - lse).  A wave holds its keys in registers
 // and goes through the rows 32 at a time, which the block brings to LDS while it works on those before.  Sums in 32 bits, those
-// of 16 tiles of rows by themselves.
+// of 16 stages of rows by themselves (up to 1024 rows).
+// Bound by exponentials and products, which overlap little: two causal prompts of 9216, 28 + 4 heads of 128 in bf16, 705 us where the
+// products alone would take 446 (the matrix cores are busy 37 % of the time, the vector units 50 %); 637 causal tokens of 32 heads in 32 bits
+// 31 with the join, by keys and rows of short blocks one after the other.
 template <int DT, int DP, class HELD>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_gather_weights(Gather a, Cache c, Shares sp, unsigned first) {
   typedef GatherShape<DT, DP> S;
